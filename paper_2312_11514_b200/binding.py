@@ -18,6 +18,11 @@ LIF_OK, LIF_ERR_INVALID_ARG, LIF_ERR_ALIGNMENT, LIF_ERR_CAPACITY, LIF_ERR_STATE,
 CNT_LEN = 64
 ACT_RELU, ACT_RELU_SQUARED, ACT_FATRELU = range(3)
 GATE_NONE, GATE_BUNDLED, GATE_RESIDENT = range(3)
+TYPE_F16, TYPE_BF16 = range(2)
+NORM_NONE, NORM_RMS, NORM_LAYER = range(3)
+ROPE_NONE, ROPE_HALF, ROPE_INTERLEAVED = range(3)
+KV_CNT_STATUS, KV_CNT_FREE, KV_CNT_COPIES, KV_CNT_REFUSED = range(4)
+KV_CNT_LEN = 32
 
 EXPORTS = [
     "lif_status_str", "lif_workspace_bytes", "lif_create_layer", "lif_destroy_layer", "lif_reset",
@@ -28,6 +33,9 @@ EXPORTS = [
     "lif_sparse_ffn_static", "lif_sparse_ffn_static_status", "lif_set_tuning", "lif_profile_launch",
     "lif_read_state", "lif_snapshot_bytes", "lif_snapshot", "lif_restore", "lif_sum_peer_outputs",
     "lif_store_open", "lif_store_close", "lif_store_read", "lif_store_get_stats", "lif_decode_step_store",
+    "lif_kv_workspace_bytes", "lif_kv_create", "lif_kv_destroy", "lif_kv_get_state", "lif_kv_reset",
+    "lif_kv_reserve", "lif_kv_append", "lif_kv_attention", "lif_kv_fork", "lif_kv_load", "lif_kv_compact",
+    "lif_kv_get_stats", "lif_kv_clear_status",
 ]
 KERNELS = ("predict_z", "predict_scores", "fetch", "ffn_active", "ffn_hits", "ffn_new", "ffn_sum",
            "ffn_cache")
@@ -65,6 +73,29 @@ class Stats(C.Structure):
 class StoreStats(C.Structure):
     _fields_ = [("reads", C.c_uint64), ("bytes_read", C.c_uint64), ("bytes_requested", C.c_uint64),
                 ("seconds_reading", C.c_double), ("direct_io", C.c_int32), ("n_threads", C.c_int32)]
+
+
+class KvDesc(C.Structure):
+    _fields_ = [
+        ("n_layers", C.c_int32), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+        ("dtype", C.c_int32), ("page_tokens", C.c_int32), ("n_pages", C.c_int32), ("max_seqs", C.c_int32),
+        ("max_pages", C.c_int32), ("max_new", C.c_int32), ("window", C.c_int32), ("scale", C.c_float),
+        ("norm", C.c_int32), ("norm_eps", C.c_float), ("rope", C.c_int32), ("rope_dims", C.c_int32),
+        ("rope_scale", C.c_float), ("host_rope_freq", C.c_void_p), ("dev_pages", C.c_void_p),
+        ("dev_workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+    ]
+
+
+class KvRows(C.Structure):
+    _fields_ = [("dev", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class KvNorms(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("dev_q_weight", "dev_q_bias", "dev_k_weight", "dev_k_bias")]
+
+
+class KvState(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("counts", "lens", "n_new", "table", "refs")]
 
 
 class LifError(RuntimeError):
@@ -125,6 +156,19 @@ def lib() -> C.CDLL:
         "lif_profile_launch": [vp, i32, vp, vp, vp],
         "lif_timing_enable": [vp, i32],
         "lif_timing_read": [vp, C.POINTER(C.c_float), C.POINTER(i32)],
+        "lif_kv_workspace_bytes": [C.POINTER(KvDesc), C.POINTER(sz)],
+        "lif_kv_create": [C.POINTER(KvDesc), C.POINTER(vp)],
+        "lif_kv_destroy": [vp],
+        "lif_kv_get_state": [vp, C.POINTER(KvState)],
+        "lif_kv_reset": [vp, vp],
+        "lif_kv_reserve": [vp, vp, vp],
+        "lif_kv_append": [vp, i32, C.POINTER(KvRows), C.POINTER(KvRows), C.POINTER(KvRows), C.POINTER(KvNorms), vp, vp],
+        "lif_kv_attention": [vp, i32, vp, vp, vp],
+        "lif_kv_fork": [vp, vp, vp, vp],
+        "lif_kv_load": [vp, vp, vp, vp, vp],
+        "lif_kv_compact": [vp, vp],
+        "lif_kv_get_stats": [vp, vp],
+        "lif_kv_clear_status": [vp, vp],
     }
     for name, args in sigs.items():
         fn = getattr(L, name)
@@ -388,3 +432,82 @@ def lif_snapshot(layer: int) -> bytes:
 def lif_restore(layer: int, snapshot: bytes) -> None:
     buf = C.create_string_buffer(snapshot, len(snapshot))
     _check(lib().lif_restore(layer, C.cast(buf, C.c_void_p), len(snapshot)), "lif_restore")
+
+
+def make_kv_desc(*, n_layers, n_heads, n_kv_heads, head_dim, page_tokens, n_pages, max_seqs, max_pages,
+                 max_new=1, dtype=TYPE_F16, window=0, scale=0.0, norm=NORM_NONE, norm_eps=0.0, rope=ROPE_NONE,
+                 rope_dims=0, rope_scale=1.0, rope_freq=None, pages=None, workspace=None) -> KvDesc:
+    """``rope_freq``: a ctypes array of doubles, alive until lif_kv_create has returned."""
+    d = KvDesc()
+    d.n_layers, d.n_heads, d.n_kv_heads, d.head_dim, d.dtype = n_layers, n_heads, n_kv_heads, head_dim, dtype
+    d.page_tokens, d.n_pages, d.max_seqs, d.max_pages, d.max_new = page_tokens, n_pages, max_seqs, max_pages, max_new
+    d.window, d.scale, d.norm, d.norm_eps = window, scale, norm, norm_eps
+    d.rope, d.rope_dims, d.rope_scale = rope, rope_dims, rope_scale
+    d.host_rope_freq = None if rope_freq is None else C.addressof(rope_freq)
+    d.dev_pages, d.dev_workspace = _ptr(pages), _ptr(workspace)
+    d.workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return d
+
+
+def lif_kv_workspace_bytes(desc: KvDesc) -> int:
+    out = C.c_size_t(0)
+    _check(lib().lif_kv_workspace_bytes(C.byref(desc), C.byref(out)), "lif_kv_workspace_bytes")
+    return out.value
+
+
+def lif_kv_create(desc: KvDesc) -> int:
+    out = C.c_void_p(None)
+    _check(lib().lif_kv_create(C.byref(desc), C.byref(out)), "lif_kv_create")
+    return out.value
+
+
+def lif_kv_destroy(kv: int) -> None:
+    _check(lib().lif_kv_destroy(kv), "lif_kv_destroy")
+
+
+def lif_kv_get_state(kv: int) -> KvState:
+    out = KvState()
+    _check(lib().lif_kv_get_state(kv, C.byref(out)), "lif_kv_get_state")
+    return out
+
+
+def lif_kv_reset(kv: int, stream=None) -> None:
+    _check(lib().lif_kv_reset(kv, _stream(stream)), "lif_kv_reset")
+
+
+def lif_kv_reserve(kv: int, n_new, stream=None) -> None:
+    _check(lib().lif_kv_reserve(kv, _ptr(n_new), _stream(stream)), "lif_kv_reserve")
+
+
+def lif_kv_append(kv: int, layer: int, q: KvRows, k: KvRows, v: KvRows, norms: Optional[KvNorms], q_out,
+                  stream=None) -> None:
+    _check(lib().lif_kv_append(kv, layer, C.byref(q), C.byref(k), C.byref(v),
+                               None if norms is None else C.byref(norms), _ptr(q_out), _stream(stream)),
+           "lif_kv_append")
+
+
+def lif_kv_attention(kv: int, layer: int, q, out, stream=None) -> None:
+    _check(lib().lif_kv_attention(kv, layer, _ptr(q), _ptr(out), _stream(stream)), "lif_kv_attention")
+
+
+def lif_kv_fork(kv: int, src=None, length=None, stream=None) -> None:
+    _check(lib().lif_kv_fork(kv, _ptr(src), _ptr(length), _stream(stream)), "lif_kv_fork")
+
+
+def lif_kv_load(kv: int, lens, table, n_new=None, stream=None) -> None:
+    _check(lib().lif_kv_load(kv, _ptr(lens), _ptr(table), _ptr(n_new), _stream(stream)), "lif_kv_load")
+
+
+def lif_kv_compact(kv: int, stream=None) -> None:
+    _check(lib().lif_kv_compact(kv, _stream(stream)), "lif_kv_compact")
+
+
+def lif_kv_get_stats(kv: int):
+    """The counts block as a list of KV_CNT_LEN ints (synchronises the device)."""
+    out = (C.c_int32 * KV_CNT_LEN)()
+    _check(lib().lif_kv_get_stats(kv, C.cast(out, C.c_void_p)), "lif_kv_get_stats")
+    return list(out)
+
+
+def lif_kv_clear_status(kv: int, stream=None) -> None:
+    _check(lib().lif_kv_clear_status(kv, _stream(stream)), "lif_kv_clear_status")

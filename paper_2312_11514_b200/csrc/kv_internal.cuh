@@ -1,0 +1,107 @@
+// Internal declarations of the paged key-value cache (lif_kv.h): kv.cu (calls and tables),
+// kv_append.cu, kv_attention.cu.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "lif_internal.cuh"
+#include "lif_kv.h"
+
+namespace lif {
+
+constexpr int kKvTile = 64;          // keys per tile of the attention kernel
+constexpr int kKvMaxCtas = 320;      // its CTAs, at most
+constexpr int kKvPlanThreads = 1024; // threads of the kernels that change the tables
+constexpr int kKvCluster = 8;        // CTAs of those that work on whole tables
+
+// Private entries of the counts block.
+enum {
+  KV_FREE_FROM = 16,      // no free page has a lower id
+  KV_TILES = 17,          // the step's attention: tiles in all,
+  KV_TILES_PER_CTA = 18,  // per CTA,
+  KV_JOINS = 19           // and entries of `joins`
+};
+
+// Everything the kernels need of a cache, by value.
+struct KvView {
+  int32_t *counts, *lens, *n_new, *table, *refs;
+  int32_t *table_tmp;      // [max_seqs][max_pages]
+  int32_t *page_tmp;       // [n_pages] scratch per page
+  int32_t *list_a, *list_b;  // [n_pages] lists of page ids; copies: source, destination ...
+  int32_t *copy_tokens;    // [n_pages] ... and rows
+  int4 *seq_plan;          // [max_seqs] {first tile, tokens, new tokens, tiles per row block}
+  int4 *cta_plan;          // [kKvMaxCtas] {place, its first tile, tokens, new tokens} at the CTA's first tile
+  int4 *joins;             // [kKvMaxCtas] {first CTA, last CTA, place, head * row blocks + row block}
+  const uint64_t* turns;   // [rope_dims/2] 2^64ths of a turn per position
+  float* partials;         // [2 * CTAs] x {[rows][head_dim], [rows] max, [rows] sum}
+  int max_seqs, max_pages, n_pages, max_new, page_shift, window;
+  int n_heads, n_kv_heads, group, head_dim, rows_per_block, ctas;
+};
+
+struct KvWorkspace {
+  size_t counts, lens, n_new, table, table_tmp, refs, page_tmp, list_a, list_b, copy_tokens,
+      seq_plan, cta_plan, joins, turns, partials, total;
+};
+
+}  // namespace lif
+
+struct lif_kv {
+  lif_kv_desc desc;
+  lif::KvView v;
+  int device, n_sm;
+  int row_tiles;            // 16-row tiles per row block of the attention kernel
+  float scale;
+};
+
+namespace lif {
+
+// elements of one page of one layer
+inline size_t kv_page_elems(const lif_kv_desc& d) {
+  return (size_t)2 * d.n_kv_heads * d.page_tokens * d.head_dim;
+}
+int kv_row_tiles(const lif_kv_desc& d);
+// CTAs per SM of the attention kernel for this cache (0: it cannot run)
+cudaError_t kv_attention_configure(const lif_kv* kv, int* ctas_per_sm);
+cudaError_t launch_kv_append(const lif_kv* kv, int layer, const lif_kv_rows& q, const lif_kv_rows& k,
+                             const lif_kv_rows& v, const lif_kv_norms& norms, void* q_out, cudaStream_t st);
+cudaError_t launch_kv_attention(const lif_kv* kv, int layer, const void* q, void* out, cudaStream_t st);
+
+#ifdef __CUDACC__
+__device__ __forceinline__ int kv_pages_of(int tokens, int shift) {
+  return (int)(((unsigned)tokens + (1u << shift) - 1) >> shift);
+}
+// First key that any of the sequence's new tokens sees, and the tiles from there on.
+__device__ __forceinline__ int kv_first_key(int tokens, int n_new, int window) {
+  const int first = tokens - n_new + 1 - window;
+  return window > 0 && first > 0 ? first : 0;
+}
+__device__ __forceinline__ int kv_tiles(int tokens, int n_new, int window) {
+  return n_new > 0 ? (tokens + kKvTile - 1) / kKvTile - kv_first_key(tokens, n_new, window) / kKvTile : 0;
+}
+__device__ __forceinline__ int kv_row_blocks(int n_new, int group, int rows_per_block) {
+  return (n_new * group + rows_per_block - 1) / rows_per_block;
+}
+
+// The two 16-bit types.
+template <typename T> struct Num;
+template <> struct Num<__half> {
+  static __device__ __forceinline__ float2 to2(uint32_t v) { return __half22float2(*reinterpret_cast<__half2*>(&v)); }
+  static __device__ __forceinline__ uint32_t from2(float a, float b) {
+    __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<uint32_t*>(&h);
+  }
+  static __device__ __forceinline__ float to1(unsigned short v) { return __half2float(__ushort_as_half(v)); }
+  static constexpr uint32_t kExponent = 0x7c007c00u;   // all ones: infinite or NaN
+};
+template <> struct Num<__nv_bfloat16> {
+  static __device__ __forceinline__ float2 to2(uint32_t v) { return __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&v)); }
+  static __device__ __forceinline__ uint32_t from2(float a, float b) {
+    __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<uint32_t*>(&h);
+  }
+  static __device__ __forceinline__ float to1(unsigned short v) { return __bfloat162float(__ushort_as_bfloat16(v)); }
+  static constexpr uint32_t kExponent = 0x7f807f80u;
+};
+#endif
+
+}  // namespace lif

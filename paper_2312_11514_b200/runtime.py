@@ -3,7 +3,9 @@
 inside the workspace as tensor views.  No arithmetic of the method lives here."""
 from __future__ import annotations
 
-from typing import Dict, List, Optional
+import ctypes as C
+import math
+from typing import Dict, List, Optional, Sequence
 
 import torch
 
@@ -105,6 +107,192 @@ class Layer:
             self.handle = None
             if not intact:
                 raise RuntimeError("a kernel wrote past the end of the cache or of the workspace")
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def rope_frequencies(dims: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                     context: int = 0, turns: Sequence[float] = (1.0, 32.0)) -> List[float]:
+    """Radians per position of the ``dims / 2`` rotated pairs, base^(-2i / dims), for contexts
+    ``factor`` times as long as ``context``, which the model was trained on:
+
+    * ``"linear"``: every frequency divided by the factor;
+    * ``"ntk"``: the base raised to base * factor^(dims / (dims - 2)): the lowest frequency is divided
+      by the factor, the highest stays;
+    * ``"by_parts"``: pairs with less than ``turns[0]`` turns in ``context`` positions divided by the
+      factor, those with more than ``turns[1]`` as they are, a linear blend in between (the usual
+      ``rope_scale`` beside it is 0.1 ln(factor) + 1)."""
+    if dims < 2 or dims % 2 or not base > 0 or not factor >= 1:
+        raise ValueError(f"rope_frequencies: dims={dims}, base={base}, factor={factor}")
+    if scaling == "ntk":
+        base = base * factor ** (dims / (dims - 2)) if dims > 2 else base
+    elif scaling == "by_parts":
+        if context < 1 or not turns[0] < turns[1]:
+            raise ValueError("rope_frequencies: by_parts needs the trained context and turns[0] < turns[1]")
+    elif scaling not in ("none", "linear"):
+        raise ValueError(f"rope_frequencies: scaling {scaling!r}")
+    out = []
+    for i in range(dims // 2):
+        f = base ** (-2.0 * i / dims)
+        if scaling == "linear":
+            f /= factor
+        elif scaling == "by_parts":
+            share = (context * f / (2 * math.pi) - turns[0]) / (turns[1] - turns[0])
+            share = min(1.0, max(0.0, share))
+            f = f * share + f / factor * (1.0 - share)
+        out.append(f)
+    return out
+
+
+class KvCache:
+    """A paged key-value cache for the attention between the FFN layers (include/lif_kv.h): owns its
+    workspace (and the pool, unless ``pages`` is given) and the handle.  Tensors are checked here for
+    device, type and shape; the calls run on ``stream``, by default the current stream of the cache's
+    device.  All calls of one cache are to be ordered (one stream, or events between streams).
+
+    ``pages``: the pool, ``[n_layers][n_pages][2][n_kv_heads][page_tokens][head_dim]``; ``lens``,
+    ``n_new``, ``table``, ``refs``: views of the tables on the device."""
+
+    _TYPES = {torch.float16: B.TYPE_F16, torch.bfloat16: B.TYPE_BF16}
+
+    def __init__(self, *, n_layers: int, n_heads: int, n_kv_heads: int, head_dim: int, n_pages: int, max_seqs: int,
+                 max_pages: Optional[int] = None, page_tokens: int = 64, max_new: int = 1, dtype=torch.float16,
+                 window: int = 0, scale: Optional[float] = None, norm: int = B.NORM_NONE, norm_eps: float = 1e-5,
+                 rope: int = B.ROPE_NONE, rope_dims: int = 0, rope_freq: Optional[Sequence[float]] = None,
+                 rope_scale: float = 1.0, pages: Optional[torch.Tensor] = None, device="cuda:0"):
+        if not torch.cuda.is_available():
+            raise RuntimeError("paper_2312_11514_b200 needs a CUDA device; there is no CPU path")
+        if dtype not in self._TYPES:
+            raise ValueError(f"KvCache: dtype {dtype} (float16 or bfloat16)")
+        self.device = torch.device(device if pages is None else pages.device)
+        self.dtype, self.max_seqs, self.max_new, self.norm = dtype, max_seqs, max_new, norm
+        self.n_heads, self.n_kv_heads, self.head_dim, self.n_layers = n_heads, n_kv_heads, head_dim, n_layers
+        self.max_pages = n_pages if max_pages is None else max_pages
+        shape = dict(n_layers=n_layers, n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim,
+                     dtype=self._TYPES[dtype], page_tokens=page_tokens, n_pages=n_pages, max_seqs=max_seqs,
+                     max_pages=self.max_pages, max_new=max_new, window=window, scale=scale or 0.0, norm=norm,
+                     norm_eps=norm_eps, rope=rope, rope_dims=rope_dims if rope != B.ROPE_NONE else 0,
+                     rope_scale=rope_scale)
+        nbytes = B.lif_kv_workspace_bytes(B.make_kv_desc(**shape))
+        pool = (n_layers, n_pages, 2, n_kv_heads, page_tokens, head_dim)
+        if pages is None:
+            pages = torch.zeros(pool, dtype=dtype, device=self.device)
+        self._expect("pages", pages, pool)
+        self.pages = pages
+        freq = None
+        if rope != B.ROPE_NONE:
+            if rope_freq is None or len(rope_freq) != rope_dims // 2:
+                raise ValueError(f"KvCache: rope_freq holds rope_dims / 2 = {rope_dims // 2} frequencies")
+            freq = (C.c_double * len(rope_freq))(*rope_freq)
+        # a guard block past the workspace, as for Layer
+        self._workspace_all = torch.zeros(nbytes + 256, dtype=torch.uint8, device=self.device)
+        self._workspace_all[nbytes:].fill_(self._GUARD)
+        self.workspace = self._workspace_all[:nbytes]
+        with torch.cuda.device(self.device):
+            torch.cuda.synchronize()
+            self.handle = B.lif_kv_create(B.make_kv_desc(**shape, rope_freq=freq, pages=pages, workspace=self.workspace))
+        state = B.lif_kv_get_state(self.handle)
+        view = lambda at, n: self.workspace[at - self.workspace.data_ptr():][:4 * n].view(torch.int32)
+        self.counts = view(state.counts, B.KV_CNT_LEN)
+        self.lens, self.n_new = view(state.lens, max_seqs), view(state.n_new, max_seqs)
+        self.table = view(state.table, max_seqs * self.max_pages).view(max_seqs, self.max_pages)
+        self.refs = view(state.refs, n_pages)
+
+    _GUARD = 0x7B
+
+    def _expect(self, name, t, shape, dtype=None, contiguous=True):
+        if t.device != self.device or t.dtype != (dtype or self.dtype) or tuple(t.shape) != tuple(shape) or \
+                (contiguous and not t.is_contiguous()):
+            raise ValueError(f"KvCache: {name} is {tuple(t.shape)} {t.dtype} on {t.device}"
+                             f"{'' if t.is_contiguous() else ', not contiguous'}; expected {tuple(shape)} "
+                             f"{dtype or self.dtype} on {self.device}")
+
+    def _ints(self, name, t, shape=None):
+        if t is not None:
+            self._expect(name, t, shape or (self.max_seqs,), torch.int32)
+        return t
+
+    def _on(self, stream):
+        return torch.cuda.current_stream(self.device) if stream is None else stream
+
+    def _rows(self, name, t, heads):
+        self._expect(name, t, (self.max_seqs, self.max_new, heads, self.head_dim), contiguous=False)
+        # places lie max_new tokens apart
+        if t.stride(3) != 1 or (self.max_seqs > 1 and self.max_new > 1 and t.stride(0) != self.max_new * t.stride(1)):
+            raise ValueError(f"KvCache: {name} has strides {t.stride()}; places have to lie max_new tokens apart, "
+                             f"a head's elements beside each other")
+        # (torch leaves the stride of a dimension of one element undefined)
+        step = t.stride(1) if self.max_new > 1 else t.stride(0) if self.max_seqs > 1 else 0
+        return B.KvRows(t.data_ptr(), step, t.stride(2) if heads > 1 else 0)
+
+    def reserve(self, n_new: torch.Tensor, stream=None) -> None:
+        B.lif_kv_reserve(self.handle, self._ints("n_new", n_new), self._on(stream))
+
+    def append(self, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_out: Optional[torch.Tensor] = None,
+               norms: Optional[Sequence[Optional[torch.Tensor]]] = None, stream=None) -> torch.Tensor:
+        """q ``[max_seqs][max_new][n_heads][head_dim]``, k and v with n_kv_heads; views into a fused
+        projection's output are fine.  ``norms``: query weight, query bias, key weight, key bias.
+        Returns the normed and rotated queries (rows of tokens that are not there are not written)."""
+        if q_out is None:
+            q_out = torch.empty(self.max_seqs, self.max_new, self.n_heads, self.head_dim, dtype=self.dtype,
+                                device=self.device)
+        else:
+            self._expect("q_out", q_out, (self.max_seqs, self.max_new, self.n_heads, self.head_dim))
+        weights = None
+        if self.norm != B.NORM_NONE and norms is not None:
+            for t in norms:
+                if t is not None:
+                    self._expect("norm weight", t, (self.head_dim,))
+            weights = B.KvNorms(*[None if t is None else t.data_ptr() for t in norms])
+        B.lif_kv_append(self.handle, layer, self._rows("q", q, self.n_heads), self._rows("k", k, self.n_kv_heads),
+                        self._rows("v", v, self.n_kv_heads), weights, q_out, self._on(stream))
+        return q_out
+
+    def attention(self, layer: int, q: torch.Tensor, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        shape = (self.max_seqs, self.max_new, self.n_heads, self.head_dim)
+        self._expect("q", q, shape)
+        if out is None:
+            out = torch.empty_like(q)
+        else:
+            self._expect("out", out, shape)
+        B.lif_kv_attention(self.handle, layer, q, out, self._on(stream))
+        return out
+
+    def fork(self, src: Optional[torch.Tensor] = None, length: Optional[torch.Tensor] = None, stream=None) -> None:
+        B.lif_kv_fork(self.handle, self._ints("src", src), self._ints("length", length), self._on(stream))
+
+    def load(self, lens: torch.Tensor, table: torch.Tensor, n_new: Optional[torch.Tensor] = None, stream=None) -> None:
+        B.lif_kv_load(self.handle, self._ints("lens", lens), self._ints("table", table, (self.max_seqs, self.max_pages)),
+                      self._ints("n_new", n_new), self._on(stream))
+
+    def compact(self, stream=None) -> None:
+        B.lif_kv_compact(self.handle, self._on(stream))
+
+    def reset(self, stream=None) -> None:
+        B.lif_kv_reset(self.handle, self._on(stream))
+
+    def clear_status(self, stream=None) -> None:
+        B.lif_kv_clear_status(self.handle, self._on(stream))
+
+    def stats(self) -> Dict[str, int]:
+        """Status, free pages, pages copied by the last call, calls refused (synchronises)."""
+        with torch.cuda.device(self.device):
+            c = B.lif_kv_get_stats(self.handle)
+        return dict(status=c[B.KV_CNT_STATUS], free=c[B.KV_CNT_FREE], copies=c[B.KV_CNT_COPIES],
+                    refused=c[B.KV_CNT_REFUSED])
+
+    def close(self) -> None:
+        if getattr(self, "handle", None):
+            torch.cuda.synchronize(self.device)
+            intact = bool((self._workspace_all[self.workspace.numel():] == self._GUARD).all())
+            B.lif_kv_destroy(self.handle)
+            self.handle = None
+            if not intact:
+                raise RuntimeError("a kernel wrote past the end of the workspace")
 
     def __del__(self):
         try:
