@@ -62,8 +62,7 @@ __device__ unsigned long long block_scan(unsigned long long x, unsigned long lon
 
 // The work of the step's attention calls, the same for every layer: tiles of kKvTile keys, in the
 // order place, key-value head, row block, tile; every CTA takes an equal run of them.  Thread b
-// holds place b's tokens.  An item (all tiles of a head and row block) that a CTA boundary cuts is
-// entered in `joins`.
+// holds place b's tokens.
 __device__ void kv_plan(const KvView& v, int tokens, int n_new) {
   __shared__ int first[kKvPlanThreads];
   __shared__ int4 place[kKvPlanThreads];
@@ -78,8 +77,6 @@ __device__ void kv_plan(const KvView& v, int tokens, int n_new) {
   if (b < v.max_seqs) v.seq_plan[b] = place[b];
   __syncthreads();
   const int q = (total + v.ctas - 1) / v.ctas;
-  int4 join = make_int4(0, 0, 0, 0);
-  bool cut = false;
   if (b < v.ctas && (long long)b * q < total) {
     const int g = b * q;
     int lo = 0, hi = v.max_seqs;              // last place whose first tile is <= g
@@ -89,17 +86,10 @@ __device__ void kv_plan(const KvView& v, int tokens, int n_new) {
     }
     const int4 p = place[lo];
     v.cta_plan[b] = make_int4(lo, p.x, p.y, p.z);
-    const int item = (g - p.x) / p.w, s = p.x + item * p.w;
-    cut = s < g && b == s / q + 1;
-    join = make_int4(b - 1, (s + p.w - 1) / q, lo, item);
   }
-  unsigned long long n_cut;
-  const int j = (int)block_scan(cut, &n_cut);
-  if (cut) v.joins[j] = join;
   if (b == 0) {
     v.counts[KV_TILES] = total;
     v.counts[KV_TILES_PER_CTA] = q;
-    v.counts[KV_JOINS] = (int)n_cut;
   }
 }
 
@@ -378,12 +368,14 @@ __global__ void __launch_bounds__(kKvPlanThreads) kv_reset_kernel(KvView v) {
   for (size_t i = at; i < (size_t)v.max_seqs * v.max_pages; i += step) v.table[i] = -1;
   for (size_t i = at; i < (size_t)v.n_pages; i += step) v.refs[i] = 0;
   if (at < (size_t)v.max_seqs) v.lens[at] = v.n_new[at] = 0;
+  if (at < kKvMaxCtas) v.tickets[at] = 0;
   if (at < LIF_KV_CNT_LEN) v.counts[at] = at == LIF_KV_CNT_FREE ? v.n_pages : 0;
 }
 
 __global__ void kv_clear_kernel(KvView v) {
   pdl_wait();
-  v.counts[LIF_KV_CNT_STATUS] = LIF_OK;
+  if (threadIdx.x == 0) v.counts[LIF_KV_CNT_STATUS] = LIF_OK;
+  if (threadIdx.x < kKvMaxCtas) v.tickets[threadIdx.x] = 0;   // a wait that ran out may have left some
 }
 
 // Rows of pages list_a[i] to pages list_b[i], every layer and head.  Unit: 4 KB of one head's rows, a
@@ -479,7 +471,7 @@ KvWorkspace plan(const lif_kv_desc& d) {
   w.copy_tokens = take(pages);
   w.seq_plan = take((size_t)d.max_seqs * 16);
   w.cta_plan = take(kKvMaxCtas * 16);
-  w.joins = take(kKvMaxCtas * 16);
+  w.tickets = take(kKvMaxCtas * 4);
   w.turns = take((size_t)d.rope_dims / 2 * 8);
   w.partials = take((size_t)2 * kKvMaxCtas * 16 * kv_row_tiles(d) * (d.head_dim + 2) * 4);
   w.total = off;
@@ -564,7 +556,7 @@ lif_status lif_kv_create(const lif_kv_desc* desc, lif_kv** out) {
   v.copy_tokens = (int32_t*)(base + w.copy_tokens);
   v.seq_plan = (int4*)(base + w.seq_plan);
   v.cta_plan = (int4*)(base + w.cta_plan);
-  v.joins = (int4*)(base + w.joins);
+  v.tickets = (int32_t*)(base + w.tickets);
   v.turns = (const uint64_t*)(base + w.turns);
   v.partials = (float*)(base + w.partials);
   v.max_seqs = desc->max_seqs;
@@ -583,7 +575,7 @@ lif_status lif_kv_create(const lif_kv_desc* desc, lif_kv** out) {
   int per_sm = 0;
   bool ok = cudaGetDevice(&kv->device) == cudaSuccess &&
             cudaDeviceGetAttribute(&kv->n_sm, cudaDevAttrMultiProcessorCount, kv->device) == cudaSuccess &&
-            kv_attention_configure(kv, &per_sm) == cudaSuccess && per_sm > 0;
+            kv_attention_configure(kv, &per_sm) && per_sm > 0;
   v.ctas = ok ? kv->n_sm * per_sm < kKvMaxCtas ? kv->n_sm * per_sm : kKvMaxCtas : 0;
   ok = ok && (pairs == 0 || cudaMemcpy(base + w.turns, turns, (size_t)pairs * 8, cudaMemcpyHostToDevice) == cudaSuccess);
   ok = ok && lif_kv_reset(kv, nullptr) == LIF_OK && cudaDeviceSynchronize() == cudaSuccess;
@@ -695,7 +687,7 @@ lif_status lif_kv_get_stats(lif_kv* kv, int32_t* host_counts) {
 lif_status lif_kv_clear_status(lif_kv* kv, void* stream) {
   const lif_status s = enter(kv);
   if (s != LIF_OK) return s;
-  return done(launch_k(kv_clear_kernel, dim3(1), dim3(1), 0, (cudaStream_t)stream, 1, kv->v));
+  return done(launch_k(kv_clear_kernel, dim3(1), dim3(kKvPlanThreads), 0, (cudaStream_t)stream, 1, kv->v));
 }
 
 }  // extern "C"

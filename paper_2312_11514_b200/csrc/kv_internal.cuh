@@ -2,6 +2,7 @@
 // kv_append.cu, kv_attention.cu.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_bf16.h>
 
 #include "lif_internal.cuh"
@@ -18,8 +19,7 @@ constexpr int kKvCluster = 8;        // CTAs of those that work on whole tables
 enum {
   KV_FREE_FROM = 16,      // no free page has a lower id
   KV_TILES = 17,          // the step's attention: tiles in all,
-  KV_TILES_PER_CTA = 18,  // per CTA,
-  KV_JOINS = 19           // and entries of `joins`
+  KV_TILES_PER_CTA = 18   // and per CTA
 };
 
 // Everything the kernels need of a cache, by value.
@@ -31,7 +31,7 @@ struct KvView {
   int32_t *copy_tokens;    // [n_pages] ... and rows
   int4 *seq_plan;          // [max_seqs] {first tile, tokens, new tokens, tiles per row block}
   int4 *cta_plan;          // [kKvMaxCtas] {place, its first tile, tokens, new tokens} at the CTA's first tile
-  int4 *joins;             // [kKvMaxCtas] {first CTA, last CTA, place, head * row blocks + row block}
+  int32_t* tickets;        // [kKvMaxCtas] pieces written of the head that a CTA's run ends in; 0 between launches
   const uint64_t* turns;   // [rope_dims/2] 2^64ths of a turn per position
   float* partials;         // [2 * CTAs] x {[rows][head_dim], [rows] max, [rows] sum}
   int max_seqs, max_pages, n_pages, max_new, page_shift, window;
@@ -40,7 +40,12 @@ struct KvView {
 
 struct KvWorkspace {
   size_t counts, lens, n_new, table, table_tmp, refs, page_tmp, list_a, list_b, copy_tokens,
-      seq_plan, cta_plan, joins, turns, partials, total;
+      seq_plan, cta_plan, tickets, turns, partials, total;
+};
+
+// The pool for tensor copies: boxes of 64 columns, and of those that head_dim % 64 leaves.
+struct KvMaps {
+  CUtensorMap wide, rest;
 };
 
 }  // namespace lif
@@ -48,6 +53,7 @@ struct KvWorkspace {
 struct lif_kv {
   lif_kv_desc desc;
   lif::KvView v;
+  lif::KvMaps maps;
   int device, n_sm;
   int row_tiles;            // 16-row tiles per row block of the attention kernel
   float scale;
@@ -60,8 +66,8 @@ inline size_t kv_page_elems(const lif_kv_desc& d) {
   return (size_t)2 * d.n_kv_heads * d.page_tokens * d.head_dim;
 }
 int kv_row_tiles(const lif_kv_desc& d);
-// CTAs per SM of the attention kernel for this cache (0: it cannot run)
-cudaError_t kv_attention_configure(const lif_kv* kv, int* ctas_per_sm);
+// Tensor maps, and CTAs per SM of the attention kernel for this cache
+bool kv_attention_configure(lif_kv* kv, int* ctas_per_sm);
 cudaError_t launch_kv_append(const lif_kv* kv, int layer, const lif_kv_rows& q, const lif_kv_rows& k,
                              const lif_kv_rows& v, const lif_kv_norms& norms, void* q_out, cudaStream_t st);
 cudaError_t launch_kv_attention(const lif_kv* kv, int layer, const void* q, void* out, cudaStream_t st);
