@@ -61,8 +61,11 @@ __device__ unsigned long long block_scan(unsigned long long x, unsigned long lon
 }
 
 // The work of the step's attention calls, the same for every layer: tiles of kKvTile keys, in the
-// order place, key-value head, row block, tile; every CTA takes an equal run of them.  Thread b
-// holds place b's tokens.
+// order place, key-value head, row block, tile, cut into runs.  Every CTA has a first run.  Short work
+// (kLongRun tiles a CTA at most) is all in those; of long work they hold three quarters, and
+// what remains is cut into runs of a twentieth of a CTA's share, which CTAs take as they become free.
+// Thread b holds place b's tokens.  A head and row block that the end of a run cuts is entered in `joins`.
+constexpr int kLongRun = 15;
 __device__ void kv_plan(const KvView& v, int tokens, int n_new) {
   __shared__ int first[kKvPlanThreads];
   __shared__ int4 place[kKvPlanThreads];
@@ -76,20 +79,52 @@ __device__ void kv_plan(const KvView& v, int tokens, int n_new) {
   place[b] = make_int4(at, tokens, n_new, nt);
   if (b < v.max_seqs) v.seq_plan[b] = place[b];
   __syncthreads();
-  const int q = (total + v.ctas - 1) / v.ctas;
-  if (b < v.ctas && (long long)b * q < total) {
-    const int g = b * q;
-    int lo = 0, hi = v.max_seqs;              // last place whose first tile is <= g
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (first[mid] <= g) lo = mid; else hi = mid;
+  const int share = (total - 1) / v.ctas + 1;        // (total = 0: 1, and no run)
+  int q0 = share, q1 = share, runs, first_runs;
+  if (share > kLongRun && v.max_runs >= 6 * v.ctas) {
+    q0 = (int)(3LL * share / 4);
+    q1 = (share + 19) / 20;                          // share - q0 <= 5 q1: six runs a CTA at most
+    first_runs = v.ctas;
+    runs = first_runs + (total - first_runs * q0 + q1 - 1) / q1;
+  } else {
+    runs = first_runs = (total + q0 - 1) / q0;
+  }
+  int n_joins = 0;
+  for (int c0 = 0; c0 < runs; c0 += kKvPlanThreads) {
+    const int c = c0 + b;
+    bool cut = false;
+    int4 join = make_int4(0, 0, 0, 0);
+    if (c < runs) {
+      const int g = c < first_runs ? c * q0 : first_runs * q0 + (c - first_runs) * q1;
+      int lo = 0, hi = v.max_seqs;            // last place whose first tile is <= g
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (first[mid] <= g) lo = mid; else hi = mid;
+      }
+      const int4 p = place[lo];
+      v.run_plan[c] = make_int4(lo, p.x, p.y, p.z);
+      const int item = (g - p.x) / p.w, s = p.x + item * p.w, e = s + p.w - 1;
+      const int before = c - 1 < first_runs ? (c - 1) * q0 : first_runs * q0 + (c - 1 - first_runs) * q1;
+      cut = s < g && before <= s;             // the first run that begins inside it
+      const int last = e < first_runs * q0 ? e / q0 : first_runs + (e - first_runs * q0) / q1;
+      const int blocks = kv_row_blocks(p.z, v.group, v.rows_per_block), head = item / blocks;
+      join = make_int4((c - 1) | last << 16, lo, head << 16 | (item - head * blocks), p.z);
     }
-    const int4 p = place[lo];
-    v.cta_plan[b] = make_int4(lo, p.x, p.y, p.z);
+    if (runs > 1) {
+      unsigned long long n_cut;
+      const int j = n_joins + (int)block_scan(cut, &n_cut);
+      if (cut) v.joins[j] = join;
+      n_joins += (int)n_cut;
+    }
   }
   if (b == 0) {
     v.counts[KV_TILES] = total;
-    v.counts[KV_TILES_PER_CTA] = q;
+    v.counts[KV_FIRST_RUNS] = first_runs;
+    v.counts[KV_FIRST_TILES] = q0;
+    v.counts[KV_RUNS] = runs;
+    v.counts[KV_MORE_TILES] = q1;
+    v.counts[KV_JOINS] = n_joins;
+    v.counts[KV_TAKEN] = 0;
   }
 }
 
@@ -368,14 +403,12 @@ __global__ void __launch_bounds__(kKvPlanThreads) kv_reset_kernel(KvView v) {
   for (size_t i = at; i < (size_t)v.max_seqs * v.max_pages; i += step) v.table[i] = -1;
   for (size_t i = at; i < (size_t)v.n_pages; i += step) v.refs[i] = 0;
   if (at < (size_t)v.max_seqs) v.lens[at] = v.n_new[at] = 0;
-  if (at < kKvMaxCtas) v.tickets[at] = 0;
   if (at < LIF_KV_CNT_LEN) v.counts[at] = at == LIF_KV_CNT_FREE ? v.n_pages : 0;
 }
 
 __global__ void kv_clear_kernel(KvView v) {
   pdl_wait();
-  if (threadIdx.x == 0) v.counts[LIF_KV_CNT_STATUS] = LIF_OK;
-  if (threadIdx.x < kKvMaxCtas) v.tickets[threadIdx.x] = 0;   // a wait that ran out may have left some
+  v.counts[LIF_KV_CNT_STATUS] = LIF_OK;
 }
 
 // Rows of pages list_a[i] to pages list_b[i], every layer and head.  Unit: 4 KB of one head's rows, a
@@ -470,10 +503,10 @@ KvWorkspace plan(const lif_kv_desc& d) {
   w.list_b = take(pages);
   w.copy_tokens = take(pages);
   w.seq_plan = take((size_t)d.max_seqs * 16);
-  w.cta_plan = take(kKvMaxCtas * 16);
-  w.tickets = take(kKvMaxCtas * 4);
+  w.run_plan = take((size_t)kv_max_runs(d) * 16);
+  w.joins = take((size_t)kv_max_runs(d) * 16);
   w.turns = take((size_t)d.rope_dims / 2 * 8);
-  w.partials = take((size_t)2 * kKvMaxCtas * 16 * kv_row_tiles(d) * (d.head_dim + 2) * 4);
+  w.partials = take((size_t)2 * kv_max_runs(d) * kv_slot_rows(d) * (d.head_dim + 4) * 4);
   w.total = off;
   return w;
 }
@@ -555,8 +588,8 @@ lif_status lif_kv_create(const lif_kv_desc* desc, lif_kv** out) {
   v.list_b = (int32_t*)(base + w.list_b);
   v.copy_tokens = (int32_t*)(base + w.copy_tokens);
   v.seq_plan = (int4*)(base + w.seq_plan);
-  v.cta_plan = (int4*)(base + w.cta_plan);
-  v.tickets = (int32_t*)(base + w.tickets);
+  v.run_plan = (int4*)(base + w.run_plan);
+  v.joins = (int4*)(base + w.joins);
   v.turns = (const uint64_t*)(base + w.turns);
   v.partials = (float*)(base + w.partials);
   v.max_seqs = desc->max_seqs;
@@ -571,6 +604,9 @@ lif_status lif_kv_create(const lif_kv_desc* desc, lif_kv** out) {
   v.group = desc->n_heads / desc->n_kv_heads;
   v.head_dim = desc->head_dim;
   v.rows_per_block = 16 * kv->row_tiles;
+  v.max_runs = kv_max_runs(*desc);
+  v.slot_rows = kv_slot_rows(*desc);
+  v.slot_floats = v.slot_rows * (desc->head_dim + 4);
 
   int per_sm = 0;
   bool ok = cudaGetDevice(&kv->device) == cudaSuccess &&
@@ -687,7 +723,7 @@ lif_status lif_kv_get_stats(lif_kv* kv, int32_t* host_counts) {
 lif_status lif_kv_clear_status(lif_kv* kv, void* stream) {
   const lif_status s = enter(kv);
   if (s != LIF_OK) return s;
-  return done(launch_k(kv_clear_kernel, dim3(1), dim3(kKvPlanThreads), 0, (cudaStream_t)stream, 1, kv->v));
+  return done(launch_k(kv_clear_kernel, dim3(1), dim3(1), 0, (cudaStream_t)stream, 1, kv->v));
 }
 
 }  // extern "C"

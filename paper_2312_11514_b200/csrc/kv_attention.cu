@@ -6,11 +6,12 @@
 // mostly), in blocks of 16 x WR.  Every key and value is read once per row block; bound: HBM, until
 // rows x heads make the tensor cores or the exponentials one (a single key-value head under many query heads).
 //
-// Split.  The step's work is numbered in tiles of 64 keys (kv_plan) and every CTA takes an equal run
-// of them, across heads and sequences, so that one long sequence, many short ones and anything ragged
-// between fill the chip alike.  A head that a run's end cuts is finished from the pieces' {max, sum,
-// unnormalised output}, in the pieces' order, by the CTA that writes the last of them (a ticket per cut
-// head); a second launch for it cost 3 us of device and 2 us of host time more.
+// Split.  The step's work is numbered in tiles of 64 keys (kv_plan) and cut into runs, across heads and
+// sequences, so that one long sequence, many short ones and anything ragged between fill the chip alike.
+// Every CTA begins with a run of its own; where the work is long these cover three quarters of it and the
+// rest is taken in short runs by whoever is free (SCHEDULE_FIGURES).  A head that a run's end cuts is
+// finished by kv_join_kernel from the pieces' {max, sum, unnormalised output}.  Which run holds which tiles
+// does not depend on who takes it, and pieces are joined in their order: the same bits every time.
 //
 // Loads.  One warp feeds the others: it walks the run, reads 32 page ids at a time and moves keys and
 // values into a ring of stages with tensor copies (TMA), a copy per page, 64 columns and operand, which
@@ -43,10 +44,17 @@ struct AttendArgs {
 struct __align__(16) StageInfo {
   int b, tokens, news, k0;     // place, its tokens, its new ones, first key
   int head, row0, flags;       // key-value head, first row of the row block
-  int cut;                     // the item's first CTA, its last one << 16
+  int run;
 };
-enum { kOpens = 1, kStarts = 2, kEnds = 4, kCloses = 8 };   // first tile of a piece, of the item; last tile of the item, of a piece
+// first tile of a piece, of the head; last tile of the head, of a piece, of the CTA
+enum { kOpens = 1, kStarts = 2, kEnds = 4, kCloses = 8, kLast = 16 };
 
+// 2^x; results below 2^-126 are 0 (a weight that small is none in 16 bits)
+__device__ __forceinline__ float power(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 __device__ __forceinline__ void ldm_x4(uint32_t* r, uint32_t at) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
@@ -92,10 +100,9 @@ struct Shape {
   static constexpr int kPitch = 2 * D + 16;                              // of query rows: ldmatrix without conflicts
   static constexpr int kQuerySlot = kRows * kPitch;                      // two: the next head's arrive meanwhile
   static constexpr int kTiles = D / 8;                                   // 8-column tiles of the output
-  // the sum over the WK warps of a row: half of the tiles that a warp sums at a time
-  static constexpr int kOwn = (kTiles + WK - 1) / WK, kPart = WK > 1 ? (kOwn + 1) / 2 : 0;
-  static constexpr int kSumBytes = kWarps * kPart * 512, kJoinBytes = kWarps * 32 * 24;
-  static constexpr int kScratch = kSumBytes > kJoinBytes ? kSumBytes : kJoinBytes;
+  // the sum over the WK warps of a row: so many of a warp's rows at a time
+  static constexpr int kSumRows = D < 128 || kWarps > 4 ? 4 : 2, kSumPitch = D + 8;
+  static constexpr int kScratch = WK > 1 ? kWarps * kSumRows * kSumPitch * 4 : 0;
   static constexpr int kMaxStages = 6;
   static constexpr int kFixed = 2 * kQuerySlot + kScratch + kRows * WK * 8 + kMaxStages * (int)sizeof(StageInfo) + 256;
   // Two CTAs an SM where three stages fit twice: one computes while the other waits.
@@ -137,34 +144,36 @@ struct Cursor {
 
 struct Barriers {
   uint64_t full[6], empty[6], q_empty[2], all;
-  int last;                     // the CTA's answer to "is this the last piece?"
 };
 
 // The warp that loads.  Waits only for stages and query slots that the other warps have used.
 template <typename T, int D, int WR, int WK>
 __device__ __forceinline__ void feed(const KvMaps& maps, const KvView& V, const AttendArgs& a, unsigned char* ring,
-                                     unsigned char* queries, StageInfo* info, Barriers* bars, int g0, int n_tiles,
-                                     int per_cta) {
+                                     unsigned char* queries, StageInfo* info, Barriers* bars, int4 plan) {
   using S = Shape<D, WR, WK>;
   constexpr int kChunks = (D + 63) / 64;
   const int lane = threadIdx.x & 31;
   const int page_tokens = 1 << V.page_shift, box = min(page_tokens, kKvTile);
   const int pages_a_tile = kKvTile / box;
+  const int total = V.counts[KV_TILES], first_runs = V.counts[KV_FIRST_RUNS], first_tiles = V.counts[KV_FIRST_TILES],
+            more_tiles = V.counts[KV_MORE_TILES], n_runs = V.counts[KV_RUNS];
+  int run = blockIdx.x, next_run = 0;
+  int g = run * first_tiles, end = min(total, g + first_tiles);
   Cursor at;
-  {
-    const int4 p = V.cta_plan[blockIdx.x];
+  auto seek = [&](const int4& p) {                   // p: the run's entry of run_plan
     at.enter(V, p.x, p.z, p.w);
-    const int in = g0 - p.y, item = in / at.tiles;
+    const int in = g - p.y, item = in / at.tiles;
     at.tile = in - item * at.tiles;
     at.head = item / at.blocks;
     at.block = item - at.head * at.blocks;
-  }
+  };
+  seek(plan);
   int held_b = -1, held_from = 0, held = 0;          // 32 page ids of a place, one a lane
   int stage = 0, piece = 0;
   unsigned turn = 0;
-  bool lost = false;
+  bool lost = false, opens_run = true, last = false;
   int i = 0;
-  for (; i < n_tiles; ++i) {
+  for (; !last; ++i) {
     const int k0 = (at.first_tile + at.tile) * kKvTile, j0 = k0 >> V.page_shift;
     const int pages = kv_pages_of(at.tokens, V.page_shift), n_pages = min(pages - j0, pages_a_tile);
     if (at.b != held_b || (j0 & ~31) != held_from) {
@@ -172,14 +181,24 @@ __device__ __forceinline__ void feed(const KvMaps& maps, const KvView& V, const 
       held_from = j0 & ~31;
       held = held_from + lane < pages ? V.table[(size_t)at.b * V.max_pages + held_from + lane] : 0;
     }
-    const bool opens = i == 0 || at.tile == 0;
+    const bool opens = opens_run || at.tile == 0;
+    if (opens_run) {                                 // the run after this one; asked for long before it is needed
+      if (first_runs < n_runs && lane == 0) next_run = first_runs + atomicAdd(V.counts + KV_TAKEN, 1);
+      if (first_runs == n_runs) next_run = n_runs;
+      opens_run = false;
+    }
+    const bool ends_run = g + 1 == end;
+    if (ends_run) {
+      next_run = __shfl_sync(~0u, next_run, 0);
+      last = next_run >= n_runs;
+    }
     if (!mbar_wait(bars->empty + stage, turn ^ 1)) lost = true;
     if (opens && !mbar_wait(bars->q_empty + (piece & 1), (piece >> 1 & 1) ^ 1)) lost = true;
-    if (__any_sync(~0u, lost)) break;
+    if (__any_sync(~0u, lost)) break;                // (nothing of this tile is on its way)
     const int row0 = at.block * S::kRows, rows = min(S::kRows, at.news * V.group - row0);
     uint64_t* bar = bars->full + stage;
     if (lane == 0) {
-      const int s = g0 + i - at.tile, ends = at.tile + 1 == at.tiles;
+      const bool ends = at.tile + 1 == at.tiles;
       StageInfo n;
       n.b = at.b;
       n.tokens = at.tokens;
@@ -188,8 +207,8 @@ __device__ __forceinline__ void feed(const KvMaps& maps, const KvView& V, const 
       n.head = at.head;
       n.row0 = row0;
       n.flags = (opens ? kOpens : 0) | (at.tile == 0 ? kStarts : 0) | (ends ? kEnds : 0) |
-                (ends || i + 1 == n_tiles ? kCloses : 0);
-      n.cut = opens ? s / per_cta | (s + at.tiles - 1) / per_cta << 16 : 0;
+                (ends || ends_run ? kCloses : 0) | (last ? kLast : 0);
+      n.run = run;
       info[stage] = n;
       mbar_expect_tx(bar, n_pages * box * D * 4 + (opens ? rows * D * 2 : 0));
     }
@@ -217,7 +236,17 @@ __device__ __forceinline__ void feed(const KvMaps& maps, const KvView& V, const 
       ++piece;
     }
     if (++stage == S::kStages) stage = 0, turn ^= 1;
-    at.step(V);
+    if (!ends_run) {
+      ++g;
+      at.step(V);
+    } else if (!last) {
+      run = next_run;
+      plan = V.run_plan[run];
+      g = first_runs * first_tiles + (run - first_runs) * more_tiles;
+      end = min(total, g + more_tiles);
+      opens_run = true;
+      seek(plan);
+    }
   }
   if (lost && lane == 0) flag_timeout(V.counts + LIF_KV_CNT_STATUS);
   // nobody leaves while copies are on their way
@@ -226,90 +255,6 @@ __device__ __forceinline__ void feed(const KvMaps& maps, const KvView& V, const 
     stage = stage == 0 ? S::kStages - 1 : stage - 1;
     mbar_wait(bars->full + stage, turn);
   }
-}
-
-// What of a cut head's row the pieces hold: the CTA's threads take four columns each, `groups` of them
-// the same ones of every groups-th piece.
-template <typename T, int D, int WR, int WK, typename Sync>
-__device__ __forceinline__ bool join(const KvView& V, const AttendArgs& a, const StageInfo& at, int rows, int first, int pieces,
-                                     unsigned char* scratch, Sync sync) {
-  using S = Shape<D, WR, WK>;
-  constexpr int kN = S::kWarps * 32;
-  const size_t slot = (size_t)S::kRows * (D + 2);
-  const int units = rows * (D / 4);
-  int groups = 1;
-  while (groups < 8 && 2 * groups * units <= kN && groups < pieces) groups *= 2;
-  float4* outs = reinterpret_cast<float4*>(scratch);
-  float2* tops = reinterpret_cast<float2*>(scratch + kN * 16);
-  for (int u = threadIdx.x; u < (groups > 1 ? kN : units); u += kN) {
-    const int group = u / units, unit = u - group * units, r = unit / (D / 4), c = unit % (D / 4);
-    float m = -INFINITY, l = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (group < groups) {
-      for (int p0 = group; p0 < pieces; p0 += 8 * groups) {
-        float pm[8], pl[8];
-        float4 x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int p = p0 + e * groups;
-          pm[e] = -INFINITY;
-          pl[e] = 0.f;
-          x[e] = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (p < pieces) {                        // piece p: the first CTA's second slot, every other one's first
-            const float* from = V.partials + (size_t)(2 * (first + p) + (p == 0)) * slot;
-            pm[e] = __ldcg(from + S::kRows * D + r);
-            pl[e] = __ldcg(from + S::kRows * (D + 1) + r);
-            x[e] = __ldcg(reinterpret_cast<const float4*>(from + (size_t)r * D) + c);
-          }
-        }
-        float top = m;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) top = fmaxf(top, pm[e]);
-        const float base = top == -INFINITY ? 0.f : top, shrink = exp2f(m - base);
-        m = top;
-        l *= shrink;
-        acc = make_float4(acc.x * shrink, acc.y * shrink, acc.z * shrink, acc.w * shrink);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float w = exp2f(pm[e] - base);
-          l = fmaf(pl[e], w, l);
-          acc.x = fmaf(w, x[e].x, acc.x);
-          acc.y = fmaf(w, x[e].y, acc.y);
-          acc.z = fmaf(w, x[e].z, acc.z);
-          acc.w = fmaf(w, x[e].w, acc.w);
-        }
-      }
-    }
-    if (groups > 1) {                              // (every thread is here, once)
-      outs[u] = acc;
-      tops[u] = make_float2(m, l);
-      if (!sync()) return false;
-      if (group == 0) {
-        float top = m;
-        for (int k = 1; k < groups; ++k) top = fmaxf(top, tops[u + k * units].x);
-        const float base = top == -INFINITY ? 0.f : top;
-        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-        l = 0.f;
-        for (int k = 0; k < groups; ++k) {
-          const float2 t = tops[u + k * units];
-          const float4 x = outs[u + k * units];
-          const float w = exp2f(t.x - base);
-          l = fmaf(t.y, w, l);
-          sum.x = fmaf(w, x.x, sum.x);
-          sum.y = fmaf(w, x.y, sum.y);
-          sum.z = fmaf(w, x.z, sum.z);
-          sum.w = fmaf(w, x.w, sum.w);
-        }
-        acc = sum;
-      }
-    }
-    if (group == 0) {
-      const int t = (at.row0 + r) / V.group, h = at.row0 + r - t * V.group;
-      T* to = reinterpret_cast<T*>(a.out) + (((int64_t)at.b * V.max_new + t) * V.n_heads + at.head * V.group + h) * D + 4 * c;
-      *reinterpret_cast<uint2*>(to) = make_uint2(Num<T>::from2(acc.x / l, acc.y / l), Num<T>::from2(acc.z / l, acc.w / l));
-    }
-  }
-  return groups == 1 || sync();                    // the scratch is free again
 }
 
 template <typename T, int D, int WR, int WK>
@@ -342,12 +287,10 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
   __syncthreads();
   pdl_wait();
   pdl_trigger();
-  const int total = V.counts[KV_TILES], per_cta = V.counts[KV_TILES_PER_CTA];
-  const int g0 = blockIdx.x * per_cta;
-  if (g0 >= total) return;
-  const int n_tiles = min(total - g0, per_cta);
+  const int4 plan = V.run_plan[blockIdx.x];          // (read beside the count; of no use past it)
+  if (blockIdx.x >= V.counts[KV_FIRST_RUNS]) return;
   if (warp == S::kWarps) {
-    feed<T, D, WR, WK>(maps, V, a, smem, queries, info, bars, g0, n_tiles, per_cta);
+    feed<T, D, WR, WK>(maps, V, a, smem, queries, info, bars, plan);
     return;
   }
 
@@ -356,7 +299,7 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
   auto sync = [&]() {                                // the warps that compute; bounded as every wait
     __syncwarp();
     if (lane == 0) mbar_arrive(&bars->all);
-    return mbar_wait(&bars->all, syncs++ & 1);
+    return mbar_wait(&bars->all, syncs++ & 1, 2 * kWaitLimit);   // (a warp that still waits for a tile comes, or never will)
   };
   auto release = [&](uint64_t* bar) {
     __syncwarp();
@@ -366,24 +309,23 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
   float m[2], sum[2];                  // running maximum; this lane's share of the sum
   int upto[2];                         // last key that the row sees
   uint32_t qf[kHold ? kSteps : 1][4];
-  int stage = 0, slot = -1, rows = 0, cut = 0;
+  int stage = 0, slot = 1, rows = 0;
   bool starts = false, idle = false;
   unsigned turn = 0;
   const uint32_t ring = smem_u32(smem), q_lane = smem_u32(queries) + (wr * 16 + (lane & 15)) * S::kPitch + (lane >> 4) * 16;
   const int key_row = wk * kKeys + (lane & 7) + (lane >> 4) * 8, key_b = lane >> 3 & 1;
   const int val_row = wk * kKeys + (lane & 15), val_b = lane >> 4;
 #pragma unroll 1
-  for (int i = 0; i < n_tiles; ++i) {
+  for (bool last = false; !last;) {
     if (!mbar_wait(bars->full + stage, turn)) {
       if (lane == 0) flag_timeout(V.counts + LIF_KV_CNT_STATUS);
       return;
     }
     const StageInfo at = info[stage];
+    last = at.flags & kLast;
     if (at.flags & kOpens) {           // another head's rows
       slot ^= 1;
-      if (slot < 0) slot = 0;
       starts = at.flags & kStarts;
-      cut = at.cut;
       rows = min(S::kRows, at.news * V.group - at.row0);
       idle = WR > 1 && wr * 16 >= rows;
 #pragma unroll
@@ -423,10 +365,6 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
       const bool edge = at.k0 + kKvTile > at.tokens - at.news + 1 || (V.window > 0 && at.k0 <= at.tokens - 1 - V.window);
       const int reach = V.window > 0 ? V.window : 0x7fffffff;
       const int first = at.k0 + wk * kKeys;
-#pragma unroll
-      for (int n = 0; n < kNT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[n][e] *= a.scale_log2;
       if (edge) {
 #pragma unroll
         for (int n = 0; n < kNT; ++n)
@@ -446,13 +384,13 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
         for (int n = 0; n < kNT; ++n) top = fmaxf(top, fmaxf(s[n][2 * h], s[n][2 * h + 1]));
         top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
         top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
-        const float base = top == -INFINITY ? 0.f : top;
-        shrink[h] = exp2f(m[h] - base);
+        const float base = top == -INFINITY ? 0.f : top * a.scale_log2;
+        shrink[h] = power(fmaf(m[h], a.scale_log2, -base));
         m[h] = top;
         float add = 0.f;
 #pragma unroll
         for (int n = 0; n < kNT; ++n) {
-          w[n][h] = Num<T>::from2(exp2f(s[n][2 * h] - base), exp2f(s[n][2 * h + 1] - base));
+          w[n][h] = Num<T>::from2(power(fmaf(s[n][2 * h], a.scale_log2, -base)), power(fmaf(s[n][2 * h + 1], a.scale_log2, -base)));
           const float2 used = Num<T>::to2(w[n][h]);
           add += used.x + used.y;
         }
@@ -547,112 +485,204 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
         all[h] = sum[h] + __shfl_xor_sync(~0u, sum[h], 1);
         all[h] += __shfl_xor_sync(~0u, all[h], 2);
       }
+      const bool whole = starts && (at.flags & kEnds);
+      // a piece that began before this run, or one that goes on behind it
+      float* part = V.partials + (size_t)(2 * at.run + starts) * V.slot_floats;
+      auto token_head = [&](int r) {                 // row r's place in the output
+        const int t = (at.row0 + r) / V.group, h = at.row0 + r - t * V.group;
+        return (((int64_t)at.b * V.max_new + t) * V.n_heads + at.head * V.group + h) * D;
+      };
+      T* out = reinterpret_cast<T*>(a.out);
       if constexpr (WK > 1) {
-        // the row's WK warps: a common maximum, then every warp sums its share of the columns
-        if (t4 == 0) {
+        // The row's WK warps lay down their outputs, a few rows at a time, and each thread sums two columns.  The
+        // first wait is bounded: a warp that gave up waiting for a tile is not there.  Past it all of them are.
+        float* mine = reinterpret_cast<float*>(scratch) + warp * S::kSumRows * S::kSumPitch;
+        const float* theirs = reinterpret_cast<const float*>(scratch) + wr * WK * S::kSumRows * S::kSumPitch;
+        const int live = min(16, rows - wr * 16);
+#pragma unroll 1
+        for (int r0 = 0; r0 < 16; r0 += S::kSumRows) {
+          if (r0 && r0 >= live) break;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) stats[(wr * 16 + g + 8 * h) * WK + wk] = make_float2(m[h], all[h]);
+          for (int h = 0; h < 2; ++h) {
+            const int r = g + 8 * h - r0;
+            if (r < 0 || r >= S::kSumRows || idle) continue;
+            if (t4 == 0) stats[(wr * 16 + r0 + r) * WK + wk] = make_float2(m[h] == -INFINITY ? m[h] : m[h] * a.scale_log2, all[h]);
+#pragma unroll
+            for (int j = 0; j < kTiles; ++j)
+              *reinterpret_cast<float2*>(mine + r * S::kSumPitch + j * 8 + 2 * t4) = make_float2(o[j][2 * h], o[j][2 * h + 1]);
+          }
+          if (r0 == 0) {
+            if (!sync()) return;
+          } else {
+            asm volatile("bar.sync %0, %1;" ::"r"(1 + wr), "n"(32 * WK) : "memory");
+          }
+#pragma unroll 1
+          for (int x = wk * 32 + lane; x < S::kSumRows * D / 2; x += 32 * WK) {
+            const int r = x / (D / 2), c = 2 * (x - r * (D / 2)), row = wr * 16 + r0 + r;
+            if (row >= rows) break;
+            float2 st[WK], sum2 = make_float2(0.f, 0.f);
+            float top = -INFINITY, l = 0.f;
+#pragma unroll
+            for (int k = 0; k < WK; ++k) {
+              st[k] = stats[row * WK + k];
+              top = fmaxf(top, st[k].x);
+            }
+            const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+            for (int k = 0; k < WK; ++k) {
+              const float f = power(st[k].x - base);
+              const float2 y = *reinterpret_cast<const float2*>(theirs + (k * S::kSumRows + r) * S::kSumPitch + c);
+              l = fmaf(st[k].y, f, l);
+              sum2.x = fmaf(f, y.x, sum2.x);
+              sum2.y = fmaf(f, y.y, sum2.y);
+            }
+            if (whole) {
+              *reinterpret_cast<uint32_t*>(out + token_head(row) + c) = Num<T>::from2(sum2.x / l, sum2.y / l);
+            } else {
+              *reinterpret_cast<float2*>(part + (size_t)row * (D + 4) + c) = sum2;
+              if (c == 0) *reinterpret_cast<float2*>(part + (size_t)row * (D + 4) + D) = make_float2(top, l);
+            }
+          }
+          asm volatile("bar.sync %0, %1;" ::"r"(1 + wr), "n"(32 * WK) : "memory");
         }
-        if (!sync()) return;
+      } else {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          float2 x[WK];
-          float top = -INFINITY;
+          const int r = wr * 16 + g + 8 * h;
+          if (r >= rows) continue;
+          if (whole) {
+            T* to = out + token_head(r) + 2 * t4;
+            const float inv = 1.f / all[h];
 #pragma unroll
-          for (int k = 0; k < WK; ++k) {
-            x[k] = stats[(wr * 16 + g + 8 * h) * WK + k];
-            top = fmaxf(top, x[k].x);
+            for (int j = 0; j < kTiles; ++j)
+              *reinterpret_cast<uint32_t*>(to + j * 8) = Num<T>::from2(o[j][2 * h] * inv, o[j][2 * h + 1] * inv);
+          } else {
+            float* to = part + (size_t)r * (D + 4);
+#pragma unroll
+            for (int j = 0; j < kTiles; ++j) *reinterpret_cast<float2*>(to + j * 8 + 2 * t4) = make_float2(o[j][2 * h], o[j][2 * h + 1]);
+            if (t4 == 0) *reinterpret_cast<float2*>(to + D) = make_float2(m[h] == -INFINITY ? m[h] : m[h] * a.scale_log2, all[h]);
           }
-          const float base = top == -INFINITY ? 0.f : top, shrink = exp2f(m[h] - base);
-          all[h] = 0.f;
-#pragma unroll
-          for (int k = 0; k < WK; ++k) all[h] = fmaf(x[k].y, exp2f(x[k].x - base), all[h]);
-          m[h] = top;
-#pragma unroll
-          for (int j = 0; j < kTiles; ++j) {
-            o[j][2 * h] *= shrink;
-            o[j][2 * h + 1] *= shrink;
-          }
-        }
-        float4* box = reinterpret_cast<float4*>(scratch);
-#pragma unroll 1
-        for (int k = 1; k < WK; ++k) {
-          const int other = (wk + k) % WK;
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            if (half * S::kPart >= S::kOwn) continue;
-            if ((k > 1 || half) && !sync()) return;
-#pragma unroll
-            for (int j = 0; j < kTiles; ++j) {
-              const int in = j / WK - half * S::kPart;
-              if (in >= 0 && in < S::kPart && j % WK == other && !idle)
-                box[((wr * WK + other) * S::kPart + in) * 32 + lane] = make_float4(o[j][0], o[j][1], o[j][2], o[j][3]);
-            }
-            if (!sync()) return;
-#pragma unroll
-            for (int j = 0; j < kTiles; ++j) {
-              const int in = j / WK - half * S::kPart;
-              if (in >= 0 && in < S::kPart && j % WK == wk && !idle) {
-                const float4 x = box[(warp * S::kPart + in) * 32 + lane];
-                o[j][0] += x.x;
-                o[j][1] += x.y;
-                o[j][2] += x.z;
-                o[j][3] += x.w;
-              }
-            }
-          }
-        }
-      }
-      const bool whole = starts && (at.flags & kEnds);
-      // a piece that began before this CTA's run, or one that goes on behind it
-      float* part = V.partials + (size_t)(2 * blockIdx.x + starts) * S::kRows * (D + 2);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int r = wr * 16 + g + 8 * h;
-        if (r >= rows) continue;
-        if (whole) {
-          const int t = (at.row0 + r) / V.group, head = at.head * V.group + at.row0 + r - t * V.group;
-          T* out = reinterpret_cast<T*>(a.out) + (((int64_t)at.b * V.max_new + t) * V.n_heads + head) * D;
-          const float inv = 1.f / all[h];
-#pragma unroll
-          for (int j = 0; j < kTiles; ++j)
-            if (j % WK == wk)
-              *reinterpret_cast<uint32_t*>(out + j * 8 + 2 * t4) = Num<T>::from2(o[j][2 * h] * inv, o[j][2 * h + 1] * inv);
-        } else {
-#pragma unroll
-          for (int j = 0; j < kTiles; ++j)
-            if (j % WK == wk) *reinterpret_cast<float2*>(part + (size_t)r * D + j * 8 + 2 * t4) = make_float2(o[j][2 * h], o[j][2 * h + 1]);
-          if (wk == 0 && t4 == 0) {
-            part[S::kRows * D + r] = m[h];
-            part[S::kRows * (D + 1) + r] = all[h];
-          }
-        }
-      }
-      if (!whole) {
-        const int from = cut & 0xffff, pieces = (cut >> 16) - from + 1;
-        __threadfence();
-        if (!sync()) return;
-        if (threadIdx.x == 0) {
-          const int before = atomicAdd(V.tickets + from, 1);
-          bars->last = before == pieces - 1;
-          if (bars->last) V.tickets[from] = 0;
-          __threadfence();
-        }
-        if (!sync()) return;
-        if (bars->last) {
-          __threadfence();
-          if (!join<T, D, WR, WK>(V, a, at, rows, from, pieces, scratch, sync)) return;
         }
       }
     }
   }
 }
 
+// Finishes the heads that the runs' ends cut: some warps of a CTA per head and row, as many as there are warps
+// for, lanes along the columns, pieces dealt to the warps and joined in a fixed order.  The lists are those
+// of the step, written before the kernel ahead passed its own wait; the pieces are that kernel's.  Bound:
+// latency (a round trip for eight pieces a warp).
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads)
+kv_join_kernel(KvView V, T* out) {
+  constexpr int kWarps = kThreads / 32, kVecs = (D + 127) / 128;       // float4 of a lane
+  __shared__ float4 fold[kWarps][kVecs * 32];
+  __shared__ float2 stat[kWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int n = V.counts[KV_JOINS], slot_rows = V.slot_rows, units = n * slot_rows;
+  int split = kWarps;                                // warps of a unit
+  while (split > 1 && (long long)units * split > (long long)gridDim.x * kWarps) split /= 2;
+  const int per_cta = kWarps / split, part = warp % split;
+  bool waited = false;
+  for (int u0 = blockIdx.x * per_cta; u0 < units; u0 += gridDim.x * per_cta) {
+    const int u = u0 + warp / split;
+    int4 join = make_int4(0, 0, 0, 0);
+    int row = 0, pieces = 0, r = 0;
+    if (u < units) {
+      join = V.joins[u / slot_rows];                 // {first run, last run << 16; place; head << 16, row block; new tokens}
+      r = u % slot_rows;
+      row = (join.z & 0xffff) * V.rows_per_block + r;
+      if (row < join.w * V.group) pieces = (join.x >> 16) - (join.x & 0xffff) + 1;
+    }
+    if (!waited) pdl_wait();
+    waited = true;
+    float m = -INFINITY, l = 0.f;
+    float4 acc[kVecs];
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v) acc[v] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int p0 = part; p0 < pieces; p0 += 8 * split) {
+      float2 st[8];
+      float4 x[8][kVecs];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int p = p0 + e * split;
+        st[e] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v) x[e][v] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (p < pieces) {                            // piece p: the first run's second slot, every other one's first
+          const float* from = V.partials + (size_t)(2 * ((join.x & 0xffff) + p) + (p == 0)) * V.slot_floats + (size_t)r * (D + 4);
+          st[e] = __ldcg(reinterpret_cast<const float2*>(from + D));
+#pragma unroll
+          for (int v = 0; v < kVecs; ++v)
+            if (v * 32 + lane < D / 4) x[e][v] = __ldcg(reinterpret_cast<const float4*>(from) + v * 32 + lane);
+        }
+      }
+      float top = m;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, st[e].x);
+      const float base = top == -INFINITY ? 0.f : top, shrink = power(m - base);
+      m = top;
+      l *= shrink;
+#pragma unroll
+      for (int v = 0; v < kVecs; ++v) acc[v] = make_float4(acc[v].x * shrink, acc[v].y * shrink, acc[v].z * shrink, acc[v].w * shrink);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float f = power(st[e].x - base);
+        l = fmaf(st[e].y, f, l);
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v) {
+          acc[v].x = fmaf(f, x[e][v].x, acc[v].x);
+          acc[v].y = fmaf(f, x[e][v].y, acc[v].y);
+          acc[v].z = fmaf(f, x[e][v].z, acc[v].z);
+          acc[v].w = fmaf(f, x[e][v].w, acc[v].w);
+        }
+      }
+    }
+    if (split > 1) {
+#pragma unroll
+      for (int v = 0; v < kVecs; ++v) fold[warp][v * 32 + lane] = acc[v];
+      if (lane == 0) stat[warp] = make_float2(m, l);
+      __syncthreads();
+      if (part == 0) {
+        for (int k = 1; k < split; ++k) m = fmaxf(m, stat[warp + k].x);
+        const float base = m == -INFINITY ? 0.f : m;
+        l = 0.f;
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v) acc[v] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < split; ++k) {
+          const float f = power(stat[warp + k].x - base);
+          l = fmaf(stat[warp + k].y, f, l);
+#pragma unroll
+          for (int v = 0; v < kVecs; ++v) {
+            const float4 x = fold[warp + k][v * 32 + lane];
+            acc[v].x = fmaf(f, x.x, acc[v].x);
+            acc[v].y = fmaf(f, x.y, acc[v].y);
+            acc[v].z = fmaf(f, x.z, acc[v].z);
+            acc[v].w = fmaf(f, x.w, acc[v].w);
+          }
+        }
+      }
+    }
+    if (part == 0 && pieces > 0) {
+      const int t = row / V.group;
+      T* to = out + (((int64_t)join.y * V.max_new + t) * V.n_heads + (join.z >> 16) * V.group + row - t * V.group) * D;
+#pragma unroll
+      for (int v = 0; v < kVecs; ++v)
+        if (v * 32 + lane < D / 4)
+          reinterpret_cast<uint2*>(to)[v * 32 + lane] =
+              make_uint2(Num<T>::from2(acc[v].x / l, acc[v].y / l), Num<T>::from2(acc[v].z / l, acc[v].w / l));
+    }
+    if (split > 1) __syncthreads();
+  }
+  if (!waited) pdl_wait();
+  if (blockIdx.x == 0 && threadIdx.x == 0) V.counts[KV_TAKEN] = 0;
+}
+
 // What to do with the kernel for a type, head dimension and row tiles: few rows leave the tile's keys to more warps.
 template <typename T, int D, int WR, int WK, typename F>
 cudaError_t with(F f) {
   using S = Shape<D, WR, WK>;
-  return f(kv_attention_kernel<T, D, WR, WK>, S::kThreads, S::kSmem);
+  return f(kv_attention_kernel<T, D, WR, WK>, kv_join_kernel<T, D>, S::kThreads, S::kSmem, (T*)nullptr);
 }
 template <typename T, int D, typename F>
 cudaError_t with_rows(int row_tiles, F f) {
@@ -719,7 +749,7 @@ bool kv_attention_configure(lif_kv* kv, int* ctas_per_sm) {
   if (!encode_map(&kv->maps.wide, kv->desc, 64, CU_TENSOR_MAP_SWIZZLE_128B)) return false;
   if (rest && !encode_map(&kv->maps.rest, kv->desc, rest, rest == 16 ? CU_TENSOR_MAP_SWIZZLE_32B : CU_TENSOR_MAP_SWIZZLE_64B))
     return false;
-  return with_kernel(kv, [&](auto kernel, int threads, int smem) {
+  return with_kernel(kv, [&](auto kernel, auto, int threads, int smem, auto) {
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(ctas_per_sm, kernel, threads, smem);
     return e;
@@ -732,8 +762,10 @@ cudaError_t launch_kv_attention(const lif_kv* kv, int layer, const void* q, void
   a.out = out;
   a.scale_log2 = kv->scale * 1.4426950408889634f;
   a.layer = layer;
-  return with_kernel(kv, [&](auto kernel, int threads, int smem) {
-    return launch_k2(kernel, dim3(kv->v.ctas), dim3(threads), smem, st, 1, 1, kv->maps, kv->v, a);
+  return with_kernel(kv, [&](auto kernel, auto join, int threads, int smem, auto* type) {
+    cudaError_t e = launch_k2(kernel, dim3(kv->v.ctas), dim3(threads), smem, st, 1, 1, kv->maps, kv->v, a);
+    if (e == cudaSuccess) e = launch_k2(join, dim3(2 * kv->n_sm), dim3(kThreads), 0, st, 1, 1, kv->v, (decltype(type))out);
+    return e;
   });
 }
 

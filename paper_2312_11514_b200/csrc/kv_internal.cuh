@@ -12,6 +12,7 @@ namespace lif {
 
 constexpr int kKvTile = 64;          // keys per tile of the attention kernel
 constexpr int kKvMaxCtas = 320;      // its CTAs, at most
+constexpr int kKvMaxRuns = 2048;     // and their runs of tiles
 constexpr int kKvPlanThreads = 1024; // threads of the kernels that change the tables
 constexpr int kKvCluster = 8;        // CTAs of those that work on whole tables
 
@@ -19,7 +20,12 @@ constexpr int kKvCluster = 8;        // CTAs of those that work on whole tables
 enum {
   KV_FREE_FROM = 16,      // no free page has a lower id
   KV_TILES = 17,          // the step's attention: tiles in all,
-  KV_TILES_PER_CTA = 18   // and per CTA
+  KV_FIRST_RUNS = 18,     // runs that a CTA of the same number begins with,
+  KV_FIRST_TILES = 19,    // their tiles,
+  KV_RUNS = 20,           // runs in all,
+  KV_MORE_TILES = 21,     // tiles of the others,
+  KV_JOINS = 22,          // entries of `joins`
+  KV_TAKEN = 23           // others taken so far; 0 between calls
 };
 
 // Everything the kernels need of a cache, by value.
@@ -30,17 +36,18 @@ struct KvView {
   int32_t *list_a, *list_b;  // [n_pages] lists of page ids; copies: source, destination ...
   int32_t *copy_tokens;    // [n_pages] ... and rows
   int4 *seq_plan;          // [max_seqs] {first tile, tokens, new tokens, tiles per row block}
-  int4 *cta_plan;          // [kKvMaxCtas] {place, its first tile, tokens, new tokens} at the CTA's first tile
-  int32_t* tickets;        // [kKvMaxCtas] pieces written of the head that a CTA's run ends in; 0 between launches
+  int4 *run_plan;          // [max_runs] {place, its first tile, tokens, new tokens} at the run's first tile
+  int4 *joins;             // [max_runs] {first run, last run << 16; place; head << 16, row block; new tokens}
   const uint64_t* turns;   // [rope_dims/2] 2^64ths of a turn per position
-  float* partials;         // [2 * CTAs] x {[rows][head_dim], [rows] max, [rows] sum}
+  float* partials;         // [2 * max_runs][slot_rows] {[head_dim], max, sum, -, -}
   int max_seqs, max_pages, n_pages, max_new, page_shift, window;
   int n_heads, n_kv_heads, group, head_dim, rows_per_block, ctas;
+  int max_runs, slot_rows, slot_floats;
 };
 
 struct KvWorkspace {
   size_t counts, lens, n_new, table, table_tmp, refs, page_tmp, list_a, list_b, copy_tokens,
-      seq_plan, cta_plan, tickets, turns, partials, total;
+      seq_plan, run_plan, joins, turns, partials, total;
 };
 
 // The pool for tensor copies: boxes of 64 columns, and of those that head_dim % 64 leaves.
@@ -66,6 +73,13 @@ inline size_t kv_page_elems(const lif_kv_desc& d) {
   return (size_t)2 * d.n_kv_heads * d.page_tokens * d.head_dim;
 }
 int kv_row_tiles(const lif_kv_desc& d);
+// rows of a row block that can be there
+inline int kv_slot_rows(const lif_kv_desc& d) {
+  const int rows = d.n_heads / d.n_kv_heads * d.max_new, block = 16 * kv_row_tiles(d);
+  return rows < block ? rows : block;
+}
+// Runs of the attention kernel's work at most: where a block has few rows, further ones beside a CTA's first.
+inline int kv_max_runs(const lif_kv_desc& d) { return kv_row_tiles(d) <= 2 ? kKvMaxRuns : kKvMaxCtas; }
 // Tensor maps, and CTAs per SM of the attention kernel for this cache
 bool kv_attention_configure(lif_kv* kv, int* ctas_per_sm);
 cudaError_t launch_kv_append(const lif_kv* kv, int layer, const lif_kv_rows& q, const lif_kv_rows& k,
