@@ -61,10 +61,11 @@ __device__ unsigned long long block_scan(unsigned long long x, unsigned long lon
 }
 
 // The work of the step's attention calls, the same for every layer: tiles of kKvTile keys, in the
-// order place, key-value head, row block, tile, cut into runs.  Every CTA has a first run.  Short work
-// (kLongRun tiles a CTA at most) is all in those; of long work they hold three quarters, and
-// what remains is cut into runs of a twentieth of a CTA's share, which CTAs take as they become free.
-// Thread b holds place b's tokens.  A head and row block that the end of a run cuts is entered in `joins`.
+// order place, key-value head, row block, tile, cut into shares, one a CTA.  Short work (kLongRun tiles
+// a share at most) is done so; of a longer share three quarters are the CTA's first run, and what remains
+// is cut into further runs of a twentieth of a share, which CTAs take as they become free.  Runs are
+// numbered as they lie.  Thread b holds place b's tokens.  A head and row block that the end of a run
+// cuts is entered in `joins`.
 constexpr int kLongRun = 15;
 __device__ void kv_plan(const KvView& v, int tokens, int n_new) {
   __shared__ int first[kKvPlanThreads];
@@ -80,33 +81,42 @@ __device__ void kv_plan(const KvView& v, int tokens, int n_new) {
   if (b < v.max_seqs) v.seq_plan[b] = place[b];
   __syncthreads();
   const int share = (total - 1) / v.ctas + 1;        // (total = 0: 1, and no run)
-  int q0 = share, q1 = share, runs, first_runs;
+  const int shares = (total + share - 1) / share;
+  int q0 = share, q1 = share, more = 0, n_more = 0;
   if (share > kLongRun && v.max_runs >= 6 * v.ctas) {
     q0 = (int)(3LL * share / 4);
-    q1 = (share + 19) / 20;                          // share - q0 <= 5 q1: six runs a CTA at most
-    first_runs = v.ctas;
-    runs = first_runs + (total - first_runs * q0 + q1 - 1) / q1;
-  } else {
-    runs = first_runs = (total + q0 - 1) / q0;
+    q1 = (share + 19) / 20;                          // share - q0 <= 5 q1: six runs a share at most
+    more = (share - q0 + q1 - 1) / q1;
+    const int rest = total - (shares - 1) * share - q0;
+    n_more = (shares - 1) * more + (rest > 0 ? (rest + q1 - 1) / q1 : 0);
   }
+  const int runs = shares ? (shares - 1) * (1 + more) + 1 + n_more - (shares - 1) * more : 0;
+  auto begin_of = [&](int run) {
+    const int c = run / (1 + more), j = run - c * (1 + more);
+    return c * share + (j ? q0 + (j - 1) * q1 : 0);
+  };
+  auto run_of = [&](int tile) {
+    const int c = tile / share, in = tile - c * share;
+    return c * (1 + more) + (in < q0 ? 0 : 1 + (in - q0) / q1);
+  };
   int n_joins = 0;
   for (int c0 = 0; c0 < runs; c0 += kKvPlanThreads) {
     const int c = c0 + b;
     bool cut = false;
     int4 join = make_int4(0, 0, 0, 0);
     if (c < runs) {
-      const int g = c < first_runs ? c * q0 : first_runs * q0 + (c - first_runs) * q1;
+      const int g = begin_of(c);
       int lo = 0, hi = v.max_seqs;            // last place whose first tile is <= g
       while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
         if (first[mid] <= g) lo = mid; else hi = mid;
       }
       const int4 p = place[lo];
-      v.run_plan[c] = make_int4(lo, p.x, p.y, p.z);
+      const int in = c % (1 + more), share_of = c / (1 + more);
+      v.run_plan[in ? v.ctas + share_of * more + in - 1 : share_of] = make_int4(lo, p.x, p.y, p.z);
       const int item = (g - p.x) / p.w, s = p.x + item * p.w, e = s + p.w - 1;
-      const int before = c - 1 < first_runs ? (c - 1) * q0 : first_runs * q0 + (c - 1 - first_runs) * q1;
-      cut = s < g && before <= s;             // the first run that begins inside it
-      const int last = e < first_runs * q0 ? e / q0 : first_runs + (e - first_runs * q0) / q1;
+      cut = s < g && begin_of(c - 1) <= s;    // the first run that begins inside it
+      const int last = run_of(e);
       const int blocks = kv_row_blocks(p.z, v.group, v.rows_per_block), head = item / blocks;
       join = make_int4((c - 1) | last << 16, lo, head << 16 | (item - head * blocks), p.z);
     }
@@ -119,10 +129,12 @@ __device__ void kv_plan(const KvView& v, int tokens, int n_new) {
   }
   if (b == 0) {
     v.counts[KV_TILES] = total;
-    v.counts[KV_FIRST_RUNS] = first_runs;
+    v.counts[KV_SHARES] = shares;
+    v.counts[KV_SHARE] = share;
     v.counts[KV_FIRST_TILES] = q0;
-    v.counts[KV_RUNS] = runs;
     v.counts[KV_MORE_TILES] = q1;
+    v.counts[KV_MORE] = more;
+    v.counts[KV_MORE_IN_ALL] = n_more;
     v.counts[KV_JOINS] = n_joins;
     v.counts[KV_TAKEN] = 0;
   }
@@ -503,7 +515,7 @@ KvWorkspace plan(const lif_kv_desc& d) {
   w.list_b = take(pages);
   w.copy_tokens = take(pages);
   w.seq_plan = take((size_t)d.max_seqs * 16);
-  w.run_plan = take((size_t)kv_max_runs(d) * 16);
+  w.run_plan = take((size_t)(kKvMaxCtas + kv_max_runs(d)) * 16);
   w.joins = take((size_t)kv_max_runs(d) * 16);
   w.turns = take((size_t)d.rope_dims / 2 * 8);
   w.partials = take((size_t)2 * kv_max_runs(d) * kv_slot_rows(d) * (d.head_dim + 4) * 4);

@@ -46,8 +46,8 @@ struct __align__(16) StageInfo {
   int head, row0, flags;       // key-value head, first row of the row block
   int run;
 };
-// first tile of a piece, of the head; last tile of the head, of a piece, of the CTA
-enum { kOpens = 1, kStarts = 2, kEnds = 4, kCloses = 8, kLast = 16 };
+// first tile of a piece, of the head; last tile of the head, of a piece, of the CTA; keys that not every row sees
+enum { kOpens = 1, kStarts = 2, kEnds = 4, kCloses = 8, kLast = 16, kEdge = 32 };
 
 // 2^x; results below 2^-126 are 0 (a weight that small is none in 16 bits)
 __device__ __forceinline__ float power(float x) {
@@ -64,12 +64,12 @@ __device__ __forceinline__ void ldm_x4_trans(uint32_t* r, uint32_t at) {
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
 }
 __device__ __forceinline__ void mma(__half, float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void mma(__nv_bfloat16, float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -97,7 +97,11 @@ struct Shape {
   static constexpr int kRows = 16 * WR, kWarps = WR * WK;
   static constexpr int kThreads = 32 * (kWarps + 1);                     // and one warp that loads
   static constexpr int kTileBytes = kKvTile * D * 2, kStage = 2 * kTileBytes;   // keys, or values; both
-  static constexpr int kPitch = 2 * D + 16;                              // of query rows: ldmatrix without conflicts
+  static constexpr bool kHold = D <= 128;                                // queries stay in registers while a head lasts
+  // Many rows come a copy per token, one behind the other, which the one ldmatrix of each pays for with
+  // conflicts; few rows, or rows read for every tile, a copy per row, 16 bytes apart.
+  static constexpr bool kDense = kHold && WR > 1;
+  static constexpr int kPitch = kDense ? 2 * D : 2 * D + 16;
   static constexpr int kQuerySlot = kRows * kPitch;                      // two: the next head's arrive meanwhile
   static constexpr int kTiles = D / 8;                                   // 8-column tiles of the output
   // the sum over the WK warps of a row: so many of a warp's rows at a time
@@ -149,16 +153,17 @@ struct Barriers {
 // The warp that loads.  Waits only for stages and query slots that the other warps have used.
 template <typename T, int D, int WR, int WK>
 __device__ __forceinline__ void feed(const KvMaps& maps, const KvView& V, const AttendArgs& a, unsigned char* ring,
-                                     unsigned char* queries, StageInfo* info, Barriers* bars, int4 plan) {
+                                     unsigned char* queries, StageInfo* info, Barriers* bars, int4 plan, int4 step) {
   using S = Shape<D, WR, WK>;
   constexpr int kChunks = (D + 63) / 64;
   const int lane = threadIdx.x & 31;
   const int page_tokens = 1 << V.page_shift, box = min(page_tokens, kKvTile);
   const int pages_a_tile = kKvTile / box;
-  const int total = V.counts[KV_TILES], first_runs = V.counts[KV_FIRST_RUNS], first_tiles = V.counts[KV_FIRST_TILES],
-            more_tiles = V.counts[KV_MORE_TILES], n_runs = V.counts[KV_RUNS];
-  int run = blockIdx.x, next_run = 0;
-  int g = run * first_tiles, end = min(total, g + first_tiles);
+  const int total = step.x, share = step.z, first_tiles = step.w;
+  const int4 others = *reinterpret_cast<const int4*>(V.counts + KV_MORE_TILES);
+  const int more_tiles = others.x, more = others.y, n_more = others.z;
+  int run = blockIdx.x * (1 + more), next = 0;
+  int g = blockIdx.x * share, end = min(total, g + first_tiles);
   Cursor at;
   auto seek = [&](const int4& p) {                   // p: the run's entry of run_plan
     at.enter(V, p.x, p.z, p.w);
@@ -183,14 +188,13 @@ __device__ __forceinline__ void feed(const KvMaps& maps, const KvView& V, const 
     }
     const bool opens = opens_run || at.tile == 0;
     if (opens_run) {                                 // the run after this one; asked for long before it is needed
-      if (first_runs < n_runs && lane == 0) next_run = first_runs + atomicAdd(V.counts + KV_TAKEN, 1);
-      if (first_runs == n_runs) next_run = n_runs;
+      if (n_more && lane == 0) next = atomicAdd(V.counts + KV_TAKEN, 1);
       opens_run = false;
     }
     const bool ends_run = g + 1 == end;
     if (ends_run) {
-      next_run = __shfl_sync(~0u, next_run, 0);
-      last = next_run >= n_runs;
+      next = __shfl_sync(~0u, next, 0);
+      last = next >= n_more;
     }
     if (!mbar_wait(bars->empty + stage, turn ^ 1)) lost = true;
     if (opens && !mbar_wait(bars->q_empty + (piece & 1), (piece >> 1 & 1) ^ 1)) lost = true;
@@ -207,7 +211,8 @@ __device__ __forceinline__ void feed(const KvMaps& maps, const KvView& V, const 
       n.head = at.head;
       n.row0 = row0;
       n.flags = (opens ? kOpens : 0) | (at.tile == 0 ? kStarts : 0) | (ends ? kEnds : 0) |
-                (ends || ends_run ? kCloses : 0) | (last ? kLast : 0);
+                (ends || ends_run ? kCloses : 0) | (last ? kLast : 0) |
+                (k0 + kKvTile > at.tokens - at.news + 1 || (V.window > 0 && k0 <= at.tokens - 1 - V.window) ? kEdge : 0);
       n.run = run;
       info[stage] = n;
       mbar_expect_tx(bar, n_pages * box * D * 4 + (opens ? rows * D * 2 : 0));
@@ -227,11 +232,18 @@ __device__ __forceinline__ void feed(const KvMaps& maps, const KvView& V, const 
     }
     if (opens) {
       unsigned char* slot = queries + (piece & 1) * S::kQuerySlot;
-      for (int r = lane; r < rows; r += 32) {
-        const int t = (row0 + r) / V.group, h = row0 + r - t * V.group;
-        bulk_g2s(slot + r * S::kPitch,
-                 reinterpret_cast<const T*>(a.q) + (((int64_t)at.b * V.max_new + t) * V.n_heads + at.head * V.group + h) * D,
-                 D * 2, bar);
+      const T* q = reinterpret_cast<const T*>(a.q) + ((int64_t)at.b * V.max_new * V.n_heads + at.head * V.group) * D;
+      const int t0 = row0 / V.group;                 // row r: head (row0 + r) % group of token (row0 + r) / group
+      if (S::kDense) {
+        for (int t = t0 + lane; t * V.group < row0 + rows; t += 32) {
+          const int r0 = max(0, t * V.group - row0), r1 = min(rows, (t + 1) * V.group - row0);
+          bulk_g2s(slot + r0 * S::kPitch, q + ((int64_t)t * V.n_heads + row0 + r0 - t * V.group) * D, (r1 - r0) * D * 2, bar);
+        }
+      } else {
+        for (int r = lane; r < rows; r += 32) {
+          const int t = (row0 + r) / V.group;
+          bulk_g2s(slot + r * S::kPitch, q + ((int64_t)t * V.n_heads + row0 + r - t * V.group) * D, D * 2, bar);
+        }
       }
       ++piece;
     }
@@ -240,10 +252,11 @@ __device__ __forceinline__ void feed(const KvMaps& maps, const KvView& V, const 
       ++g;
       at.step(V);
     } else if (!last) {
-      run = next_run;
-      plan = V.run_plan[run];
-      g = first_runs * first_tiles + (run - first_runs) * more_tiles;
-      end = min(total, g + more_tiles);
+      const int c = next / more, j = next - c * more;
+      run = c * (1 + more) + 1 + j;
+      plan = V.run_plan[V.ctas + next];
+      g = c * share + first_tiles + j * more_tiles;
+      end = min(min(total, c * share + share), g + more_tiles);
       opens_run = true;
       seek(plan);
     }
@@ -264,7 +277,7 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
   constexpr int kSteps = D / 16;                     // k steps of the first product
   constexpr int kKeys = kKvTile / WK, kNT = kKeys / 8;   // a warp's keys of a tile
   constexpr int kTiles = S::kTiles;
-  constexpr bool kHold = D <= 128;                   // the rows' queries stay in registers
+  constexpr bool kHold = S::kHold;
   extern __shared__ __align__(1024) unsigned char smem[];
   unsigned char* queries = smem + S::kStages * S::kStage;
   unsigned char* scratch = queries + 2 * S::kQuerySlot;
@@ -274,6 +287,10 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
   static_assert(sizeof(Barriers) <= 256, "");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
 
+  if (threadIdx.x == 32) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.wide) : "memory");
+    if (D % 64) asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.rest) : "memory");
+  }
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::kStages; ++i) {
       mbar_init(bars->full + i, 1);
@@ -287,10 +304,10 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
   __syncthreads();
   pdl_wait();
   pdl_trigger();
-  const int4 plan = V.run_plan[blockIdx.x];          // (read beside the count; of no use past it)
-  if (blockIdx.x >= V.counts[KV_FIRST_RUNS]) return;
+  const int4 plan = V.run_plan[blockIdx.x], step = *reinterpret_cast<const int4*>(V.counts + KV_TILES);
+  if (blockIdx.x >= step.y) return;
   if (warp == S::kWarps) {
-    feed<T, D, WR, WK>(maps, V, a, smem, queries, info, bars, plan);
+    feed<T, D, WR, WK>(maps, V, a, smem, queries, info, bars, plan, step);
     return;
   }
 
@@ -306,7 +323,7 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
     if (lane == 0) mbar_arrive(bar);
   };
   float o[kTiles][4];                  // rows g, g + 8; all columns
-  float m[2], sum[2];                  // running maximum; this lane's share of the sum
+  float m[2], sum[2];                  // what weights refer to; this lane's share of their sum
   int upto[2];                         // last key that the row sees
   uint32_t qf[kHold ? kSteps : 1][4];
   int stage = 0, slot = 1, rows = 0;
@@ -360,43 +377,76 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
           mma(T(), s[n + 1], kHold ? qf[k] : qa, kf[2], kf[3]);
         }
       }
-      // keys that not every row sees
-      const int lowest = kv_first_key(at.tokens, at.news, V.window);
-      const bool edge = at.k0 + kKvTile > at.tokens - at.news + 1 || (V.window > 0 && at.k0 <= at.tokens - 1 - V.window);
-      const int reach = V.window > 0 ? V.window : 0x7fffffff;
-      const int first = at.k0 + wk * kKeys;
-      if (edge) {
+      const int first = at.k0 + wk * kKeys, reach = V.window > 0 ? V.window : 0x7fffffff;
+      // A row's weight of a key that it does not see is 0, but 0 times an infinite or NaN value is not.
+      // Values that no row sees are cleared; where rows differ in what they see and a value is not
+      // finite, the products are formed one by one, the unseen ones left out.
+      bool one_by_one = false;
+      if (at.flags & kEdge) {
 #pragma unroll
         for (int n = 0; n < kNT; ++n)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int key = first + n * 8 + 2 * t4 + (e & 1), last = upto[e >> 1];
-            if (key > last || last - key >= reach) s[n][e] = -INFINITY;
+            const int key = first + n * 8 + 2 * t4 + (e & 1), last_seen = upto[e >> 1];
+            if (key > last_seen || last_seen - key >= reach) s[n][e] = -INFINITY;
           }
+        // keys [some, all) and [few, end) are seen by some rows, those before and behind by none
+        const int some = kv_first_key(at.tokens, at.news, V.window), all = V.window > 0 ? at.tokens - V.window : 0;
+        const int few = at.tokens - at.news + 1;
+        const bool clear = first < some || first + kKeys > at.tokens;
+        const bool differ = at.news > 1 && (first < all || first + kKeys > few);
+        if (clear || differ) {
+          constexpr int kPieces = D / 8, kLanes = kPieces <= 8 ? 8 : kPieces <= 16 ? 16 : 32;
+          const int c = lane % kLanes;
+          bool odd = false;
+          for (int k = lane / kLanes; k < kKeys; k += 32 / kLanes) {
+            const int r = wk * kKeys + k, key = first + k;
+            const bool none = key < some || key >= at.tokens;
+            if (c >= kPieces || !(none || differ)) continue;
+            uint4* v = reinterpret_cast<uint4*>(smem + (values - ring) + (c / 8 < D / 64 ? (c / 8) * 8192 + r * 128 + ((c & 7) ^ (r & 7)) * 16
+                                                                         : D % 64 == 16 ? D / 64 * 8192 + r * 32 + ((c & 1) ^ (r >> 2 & 1)) * 16
+                                                                                        : D / 64 * 8192 + r * 64 + ((c & 3) ^ (r >> 1 & 3)) * 16));
+            if (none) {
+              *v = make_uint4(0, 0, 0, 0);
+            } else {
+              const uint4 bits = *v;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const uint32_t y = (&bits.x)[e], lo = Num<T>::kExponent & 0xffffu, hi = Num<T>::kExponent & 0xffff0000u;
+                odd = odd || (y & lo) == lo || (y & hi) == hi;
+              }
+            }
+          }
+          one_by_one = __any_sync(~0u, odd);
+          __syncwarp();
+          if (clear) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the ring's copies come behind these stores
+        }
       }
-      // weights 2^(s - max); a row that has seen nothing yet keeps max = -inf and weights 0
-      uint32_t w[kNT][2];
-      float shrink[2];
+      // Weights 2^(s - m).  m need not be the maximum, only near enough that no weight is large: it is brought
+      // up to date, and what was summed scaled down, when a score lies more than kSlack above it.  The key that
+      // set m has weight 1, so nothing gets smaller than with the maximum.  A row that has seen nothing
+      // yet has m = -inf and weights 0.
+      constexpr float kSlack = 8.f;                  // weights up to 256
+      bool above = false;
+      float top[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        float top = m[h];
+        top[h] = fmaxf(s[0][2 * h], s[0][2 * h + 1]);
 #pragma unroll
-        for (int n = 0; n < kNT; ++n) top = fmaxf(top, fmaxf(s[n][2 * h], s[n][2 * h + 1]));
-        top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
-        top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
-        const float base = top == -INFINITY ? 0.f : top * a.scale_log2;
-        shrink[h] = power(fmaf(m[h], a.scale_log2, -base));
-        m[h] = top;
-        float add = 0.f;
-#pragma unroll
-        for (int n = 0; n < kNT; ++n) {
-          w[n][h] = Num<T>::from2(power(fmaf(s[n][2 * h], a.scale_log2, -base)), power(fmaf(s[n][2 * h + 1], a.scale_log2, -base)));
-          const float2 used = Num<T>::to2(w[n][h]);
-          add += used.x + used.y;
-        }
-        sum[h] = fmaf(sum[h], shrink[h], add);
+        for (int n = 1; n < kNT; ++n) top[h] = fmaxf(top[h], fmaxf(s[n][2 * h], s[n][2 * h + 1]));
+        top[h] *= a.scale_log2;
+        above = above || top[h] > m[h] + kSlack;
       }
-      if (__any_sync(~0u, shrink[0] != 1.f || shrink[1] != 1.f)) {
+      if (__any_sync(~0u, above)) {
+        float shrink[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          top[h] = fmaxf(top[h], __shfl_xor_sync(~0u, top[h], 1));
+          top[h] = fmaxf(fmaxf(top[h], __shfl_xor_sync(~0u, top[h], 2)), m[h]);
+          shrink[h] = power(m[h] - (top[h] == -INFINITY ? 0.f : top[h]));
+          m[h] = top[h];
+          sum[h] *= shrink[h];
+        }
 #pragma unroll
         for (int j = 0; j < kTiles; ++j) {
           o[j][0] *= shrink[0];
@@ -405,32 +455,16 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
           o[j][3] *= shrink[1];
         }
       }
-      // A row's weight of a key that it does not see is 0, but 0 times an infinite or NaN value is not.
-      // Values that no row sees are cleared; where rows differ in what they see and a value is not
-      // finite, the products are formed one by one, the unseen ones left out.
-      bool one_by_one = false;
-      if (edge) {
-        bool odd = false;
-#pragma unroll 1
-        for (int x = lane; x < kKeys * (D / 8); x += 32) {
-          const int r = wk * kKeys + x / (D / 8), c = x % (D / 8), key = at.k0 + r;
-          uint4* v = reinterpret_cast<uint4*>(smem + (values - ring) + (c / 8 < D / 64 ? (c / 8) * 8192 + r * 128 + ((c & 7) ^ (r & 7)) * 16
-                                                                       : D % 64 == 16 ? D / 64 * 8192 + r * 32 + ((c & 1) ^ (r >> 2 & 1)) * 16
-                                                                                      : D / 64 * 8192 + r * 64 + ((c & 3) ^ (r >> 1 & 3)) * 16));
-          if (key >= at.tokens || key < lowest) {
-            *v = make_uint4(0, 0, 0, 0);
-          } else if (at.news > 1) {
-            const uint4 bits = *v;
+      uint32_t w[kNT][2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t y = (&bits.x)[e], lo = Num<T>::kExponent & 0xffffu, hi = Num<T>::kExponent & 0xffff0000u;
-              odd = odd || (y & lo) == lo || (y & hi) == hi;
-            }
-          }
+      for (int h = 0; h < 2; ++h) {
+        const float base = m[h] == -INFINITY ? 0.f : m[h];
+#pragma unroll
+        for (int n = 0; n < kNT; ++n) {
+          w[n][h] = Num<T>::from2(power(fmaf(s[n][2 * h], a.scale_log2, -base)), power(fmaf(s[n][2 * h + 1], a.scale_log2, -base)));
+          const float2 used = Num<T>::to2(w[n][h]);
+          sum[h] += used.x + used.y;
         }
-        one_by_one = __any_sync(~0u, odd);
-        __syncwarp();
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the ring's copies come behind these stores
       }
       if (!one_by_one) {
 #pragma unroll
@@ -506,7 +540,7 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
           for (int h = 0; h < 2; ++h) {
             const int r = g + 8 * h - r0;
             if (r < 0 || r >= S::kSumRows || idle) continue;
-            if (t4 == 0) stats[(wr * 16 + r0 + r) * WK + wk] = make_float2(m[h] == -INFINITY ? m[h] : m[h] * a.scale_log2, all[h]);
+            if (t4 == 0) stats[(wr * 16 + r0 + r) * WK + wk] = make_float2(m[h], all[h]);
 #pragma unroll
             for (int j = 0; j < kTiles; ++j)
               *reinterpret_cast<float2*>(mine + r * S::kSumPitch + j * 8 + 2 * t4) = make_float2(o[j][2 * h], o[j][2 * h + 1]);
@@ -560,7 +594,7 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
             float* to = part + (size_t)r * (D + 4);
 #pragma unroll
             for (int j = 0; j < kTiles; ++j) *reinterpret_cast<float2*>(to + j * 8 + 2 * t4) = make_float2(o[j][2 * h], o[j][2 * h + 1]);
-            if (t4 == 0) *reinterpret_cast<float2*>(to + D) = make_float2(m[h] == -INFINITY ? m[h] : m[h] * a.scale_log2, all[h]);
+            if (t4 == 0) *reinterpret_cast<float2*>(to + D) = make_float2(m[h], all[h]);
           }
         }
       }
@@ -568,14 +602,15 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
   }
 }
 
+constexpr int kJoinThreads = 512;
 // Finishes the heads that the runs' ends cut: some warps of a CTA per head and row, as many as there are warps
 // for, lanes along the columns, pieces dealt to the warps and joined in a fixed order.  The lists are those
 // of the step, written before the kernel ahead passed its own wait; the pieces are that kernel's.  Bound:
 // latency (a round trip for eight pieces a warp).
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kJoinThreads)
 kv_join_kernel(KvView V, T* out) {
-  constexpr int kWarps = kThreads / 32, kVecs = (D + 127) / 128;       // float4 of a lane
+  constexpr int kWarps = kJoinThreads / 32, kVecs = (D + 127) / 128;       // float4 of a lane
   __shared__ float4 fold[kWarps][kVecs * 32];
   __shared__ float2 stat[kWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -764,7 +799,7 @@ cudaError_t launch_kv_attention(const lif_kv* kv, int layer, const void* q, void
   a.layer = layer;
   return with_kernel(kv, [&](auto kernel, auto join, int threads, int smem, auto* type) {
     cudaError_t e = launch_k2(kernel, dim3(kv->v.ctas), dim3(threads), smem, st, 1, 1, kv->maps, kv->v, a);
-    if (e == cudaSuccess) e = launch_k2(join, dim3(2 * kv->n_sm), dim3(kThreads), 0, st, 1, 1, kv->v, (decltype(type))out);
+    if (e == cudaSuccess) e = launch_k2(join, dim3(kv->n_sm), dim3(kJoinThreads), 0, st, 1, 1, kv->v, (decltype(type))out);
     return e;
   });
 }

@@ -19,13 +19,16 @@ constexpr int kKvCluster = 8;        // CTAs of those that work on whole tables
 // Private entries of the counts block.
 enum {
   KV_FREE_FROM = 16,      // no free page has a lower id
-  KV_TILES = 17,          // the step's attention: tiles in all,
-  KV_FIRST_RUNS = 18,     // runs that a CTA of the same number begins with,
-  KV_FIRST_TILES = 19,    // their tiles,
-  KV_RUNS = 20,           // runs in all,
-  KV_MORE_TILES = 21,     // tiles of the others,
-  KV_JOINS = 22,          // entries of `joins`
-  KV_TAKEN = 23           // others taken so far; 0 between calls
+  // the step's attention (kv_plan); two 16-byte loads
+  KV_TILES = 20,          // tiles in all,
+  KV_SHARES = 21,         // shares that they are cut into, one a CTA,
+  KV_SHARE = 22,          // tiles of a share,
+  KV_FIRST_TILES = 23,    // of them the CTA's first run,
+  KV_MORE_TILES = 24,     // a further run,
+  KV_MORE = 25,           // further runs of a share
+  KV_MORE_IN_ALL = 26,    // and of all (the last share may have fewer),
+  KV_JOINS = 27,          // entries of `joins`
+  KV_TAKEN = 28           // further runs taken so far; 0 between calls
 };
 
 // Everything the kernels need of a cache, by value.
@@ -36,7 +39,8 @@ struct KvView {
   int32_t *list_a, *list_b;  // [n_pages] lists of page ids; copies: source, destination ...
   int32_t *copy_tokens;    // [n_pages] ... and rows
   int4 *seq_plan;          // [max_seqs] {first tile, tokens, new tokens, tiles per row block}
-  int4 *run_plan;          // [max_runs] {place, its first tile, tokens, new tokens} at the run's first tile
+  int4 *run_plan;          // [CTAs] of their first runs, [max_runs] of the others:
+                           // {place, its first tile, tokens, new tokens} at the run's first tile
   int4 *joins;             // [max_runs] {first run, last run << 16; place; head << 16, row block; new tokens}
   const uint64_t* turns;   // [rope_dims/2] 2^64ths of a turn per position
   float* partials;         // [2 * max_runs][slot_rows] {[head_dim], max, sum, -, -}
