@@ -6,10 +6,12 @@
 // kilobytes of tables), except kv_copy_pages_kernel, which moves pages and is bound by HBM.
 //
 //   kv_reserve_kernel   once per token: one CTA, a thread per place, so that everything a place
-//                       decides sits in its thread and the shared parts are two block scans
-//   kv_arrange_kernel   fork and load: one cluster of eight CTAs; its phases are separated by the
-//                       cluster's barrier in place of launches
-//   kv_compact_kernel   likewise
+//                       decides sits in its thread and the shared parts are two block scans; three
+//                       round trips (lengths; last pages and the first free ones; references)
+//   kv_arrange_kernel   fork and load: tables of up to kSmallPages pages and kSmallTable entries in one
+//                       CTA, references counted in shared memory; larger ones in a cluster of eight, whose
+//                       barrier separates the phases in place of launches.  COMPARE_FIGURES
+//   kv_compact_kernel   likewise (kv_compact_small_kernel: one CTA, lists and new ids in shared memory)
 //   kv_copy_pages_kernel  what reserve and compact decided to copy, all layers; a warp per 4 KB
 //
 // Free pages are given out lowest id first, references are counted (integer sums, whatever order),
@@ -70,7 +72,9 @@ constexpr int kLongRun = 15;
 __device__ void kv_plan(const KvView& v, int tokens, int n_new) {
   __shared__ int first[kKvPlanThreads];
   __shared__ int4 place[kKvPlanThreads];
+  __shared__ int n_joins;
   const int b = threadIdx.x;
+  if (b == 0) n_joins = 0;
   const int nt = b < v.max_seqs ? kv_tiles(tokens, n_new, v.window) : 0;
   unsigned long long all;
   const int at = (int)block_scan(
@@ -99,34 +103,24 @@ __device__ void kv_plan(const KvView& v, int tokens, int n_new) {
     const int c = tile / share, in = tile - c * share;
     return c * (1 + more) + (in < q0 ? 0 : 1 + (in - q0) / q1);
   };
-  int n_joins = 0;
-  for (int c0 = 0; c0 < runs; c0 += kKvPlanThreads) {
-    const int c = c0 + b;
-    bool cut = false;
-    int4 join = make_int4(0, 0, 0, 0);
-    if (c < runs) {
-      const int g = begin_of(c);
-      int lo = 0, hi = v.max_seqs;            // last place whose first tile is <= g
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (first[mid] <= g) lo = mid; else hi = mid;
-      }
-      const int4 p = place[lo];
-      const int in = c % (1 + more), share_of = c / (1 + more);
-      v.run_plan[in ? v.ctas + share_of * more + in - 1 : share_of] = make_int4(lo, p.x, p.y, p.z);
-      const int item = (g - p.x) / p.w, s = p.x + item * p.w, e = s + p.w - 1;
-      cut = s < g && begin_of(c - 1) <= s;    // the first run that begins inside it
-      const int last = run_of(e);
-      const int blocks = kv_row_blocks(p.z, v.group, v.rows_per_block), head = item / blocks;
-      join = make_int4((c - 1) | last << 16, lo, head << 16 | (item - head * blocks), p.z);
+  for (int c = b; c < runs; c += kKvPlanThreads) {
+    const int g = begin_of(c);
+    int lo = 0, hi = v.max_seqs;              // last place whose first tile is <= g
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (first[mid] <= g) lo = mid; else hi = mid;
     }
-    if (runs > 1) {
-      unsigned long long n_cut;
-      const int j = n_joins + (int)block_scan(cut, &n_cut);
-      if (cut) v.joins[j] = join;
-      n_joins += (int)n_cut;
+    const int4 p = place[lo];
+    const int in = c % (1 + more), share_of = c / (1 + more);
+    v.run_plan[in ? v.ctas + share_of * more + in - 1 : share_of] = make_int4(lo, p.x, p.y, p.z);
+    const int item = (g - p.x) / p.w, s = p.x + item * p.w;
+    if (s < g && begin_of(c - 1) <= s) {      // the first run that begins inside the item
+      const int blocks = kv_row_blocks(p.z, v.group, v.rows_per_block), head = item / blocks;
+      // (where an entry stands does not matter)
+      v.joins[atomicAdd(&n_joins, 1)] = make_int4((c - 1) | run_of(s + p.w - 1) << 16, lo, head << 16 | (item - head * blocks), p.z);
     }
   }
+  __syncthreads();
   if (b == 0) {
     v.counts[KV_TILES] = total;
     v.counts[KV_SHARES] = shares;
@@ -140,9 +134,17 @@ __device__ void kv_plan(const KvView& v, int tokens, int n_new) {
   }
 }
 
+// Pages that a step can take: its tokens' and one for a copy, a place.
+static_assert(LIF_KV_MAX_SEQS <= kKvPlanThreads, "");
+int reserve_list(const KvView& v) {
+  const int n = v.max_seqs * ((v.max_new >> v.page_shift) + 2);
+  return n > kKvPlanThreads ? n : kKvPlanThreads;
+}
+constexpr int kReserveListMost = kKvPlanThreads * (LIF_KV_MAX_NEW / 8 + 2);
+
 __global__ void __launch_bounds__(kKvPlanThreads)
 kv_reserve_kernel(KvView v, const int32_t* n_new) {
-  __shared__ int shared_tail[kKvPlanThreads];
+  extern __shared__ int page_list[];         // [reserve_list]
   pdl_wait();
   const int b = threadIdx.x;
   const bool mine = b < v.max_seqs;
@@ -152,51 +154,59 @@ kv_reserve_kernel(KvView v, const int32_t* n_new) {
   const int used = kv_pages_of(tokens, v.page_shift), wanted = kv_pages_of(tokens + (bad ? 0 : n), v.page_shift);
   const int filled = tokens & ((1 << v.page_shift) - 1);
   int tail = -1, holders = 0;
-  if (!bad && n > 0 && filled) {
-    tail = v.table[(size_t)b * v.max_pages + used - 1];
-    holders = v.refs[tail];
-  }
+  if (!bad && n > 0 && filled) tail = v.table[(size_t)b * v.max_pages + used - 1];
+  // the first four times kKvPlanThreads pages that may be free: on their way beside the last pages
+  auto free_of = [&](int p) {
+    unsigned mask = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (p + i < v.n_pages && v.refs[p + i] == 0) mask |= 1u << i;
+    return mask;
+  };
+  int p0 = free_from & ~3;
+  unsigned free4 = free_of(p0 + 4 * b);
+  if (tail >= 0) holders = v.refs[tail];
   // Copy on write.  A page that several entries name and that this place is about to write behind
   // its own rows; the lowest place may go on in it where nobody is left who does not leave it.
   bool copy = holders > 1;
-  shared_tail[b] = copy ? tail : -1;
+  page_list[b] = copy ? tail : -1;
   if (__syncthreads_or(copy) && copy) {
     int growers = 0, lowest = b;
     for (int o = 0; o < v.max_seqs; ++o)
-      if (shared_tail[o] == tail) {
+      if (page_list[o] == tail) {
         ++growers;
         lowest = o < lowest ? o : lowest;
       }
     copy = !(growers == holders && lowest == b);
   }
+  // one scan: pages (up to 10 a place), copies, and what refuses the call
   const int take = wanted - used + copy;
   unsigned long long sums;
-  const unsigned long long before = block_scan((unsigned long long)take | (unsigned long long)copy << 32, &sums);
-  const int total = (int)(uint32_t)sums, n_copies = (int)(sums >> 32);
-  const int at = (int)(uint32_t)before, copy_at = (int)(before >> 32);
-  int code = __syncthreads_or(bad) ? LIF_ERR_INVALID_ARG : LIF_OK;
-  const bool full = __syncthreads_or(wanted > v.max_pages) || total > n_free;
-  if (code == LIF_OK && full) code = LIF_ERR_CAPACITY;
+  const unsigned long long before =
+      block_scan((unsigned long long)take | (unsigned long long)copy << 16 | (unsigned long long)(wanted > v.max_pages) << 32 |
+                     (unsigned long long)bad << 48, &sums);
+  const int total = (int)(sums & 0xffff), n_copies = (int)(sums >> 16 & 0xffff);
+  const int at = (int)(before & 0xffff), copy_at = (int)(before >> 16 & 0xffff);
+  int code = sums >> 48 ? LIF_ERR_INVALID_ARG : (sums >> 32 & 0xffff) || total > n_free ? LIF_ERR_CAPACITY : LIF_OK;
   // the `total` lowest free pages, four a thread and round
   if (code == LIF_OK && total > 0) {
     int found = 0;
-    for (int p0 = free_from & ~3; p0 < v.n_pages && found < total; p0 += 4 * kKvPlanThreads) {
-      const int p = p0 + 4 * b;
-      unsigned free4 = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (p + i < v.n_pages && v.refs[p + i] == 0) free4 |= 1u << i;
+    for (;;) {
       unsigned long long here;
       int r = found + (int)block_scan(__popc(free4), &here);
+      const int p = p0 + 4 * b;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         if (free4 >> i & 1) {
-          if (r < total) v.page_tmp[r] = p + i;
+          if (r < total) page_list[r] = p + i;
           ++r;
         }
       found += (int)here;
+      p0 += 4 * kKvPlanThreads;
+      if (found >= total || p0 >= v.n_pages) break;
+      free4 = free_of(p0 + 4 * b);
     }
-    __syncthreads();                       // (page_tmp: written by this block, read by it below)
+    __syncthreads();
     if (found < total) code = LIF_ERR_STATE;
   }
   if (code != LIF_OK) {
@@ -211,7 +221,7 @@ kv_reserve_kernel(KvView v, const int32_t* n_new) {
   if (mine) {
     int next = at;
     if (copy) {
-      const int page = v.page_tmp[next++];
+      const int page = page_list[next++];
       v.table[(size_t)b * v.max_pages + used - 1] = page;
       v.list_a[copy_at] = tail;
       v.list_b[copy_at] = page;
@@ -220,7 +230,7 @@ kv_reserve_kernel(KvView v, const int32_t* n_new) {
       v.refs[page] = 1;
     }
     for (int j = used; j < wanted; ++j) {
-      const int page = v.page_tmp[next++];
+      const int page = page_list[next++];
       v.table[(size_t)b * v.max_pages + j] = page;
       v.refs[page] = 1;
     }
@@ -229,84 +239,137 @@ kv_reserve_kernel(KvView v, const int32_t* n_new) {
   }
   if (b == 0) {
     v.counts[LIF_KV_CNT_FREE] = n_free - total;
-    if (total) v.counts[KV_FREE_FROM] = v.page_tmp[total - 1] + 1;
+    if (total) v.counts[KV_FREE_FROM] = page_list[total - 1] + 1;
     v.counts[LIF_KV_CNT_COPIES] = n_copies;
   }
   kv_plan(v, tokens + n, n);
 }
 
+// Table entries are handled in chunks of 32 of one row, a warp each.  The last row whose first chunk is
+// <= chunk (rows without chunks have the next one's).
+__device__ __forceinline__ int row_of_chunk(const int* first_chunk, int rows, int chunk) {
+  int lo = 0, hi = rows;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (first_chunk[mid] <= chunk) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+constexpr int kEarlyChunks = 4;              // a warp's chunks whose loads travel together and that stay in registers
+
 // What fork and load have in common: new rows of the table from given ones, references counted anew.
 // `from`: the rows' source, v.table (fork: row src[b]) or the caller's table (load: row b).
-__global__ void __cluster_dims__(kKvCluster, 1, 1) __launch_bounds__(kKvPlanThreads)
+template <bool kSmall>
+__global__ void __cluster_dims__(kSmall ? 1 : kKvCluster, 1, 1) __launch_bounds__(kKvPlanThreads)
 kv_arrange_kernel(KvView v, const int32_t* from, const int32_t* src, const int32_t* len, const int32_t* n_new, int load) {
-  __shared__ int s_src[kKvPlanThreads], s_pages[kKvPlanThreads], s_old[kKvPlanThreads];
-  __shared__ int s_bad, s_free, s_first;
+  extern __shared__ int held_by[];           // [n_pages] (small tables)
+  __shared__ int s_src[kKvPlanThreads], s_pages[kKvPlanThreads], s_all[kKvPlanThreads], s_step[kKvPlanThreads],
+      s_first[kKvPlanThreads];
+  __shared__ int s_bad, s_free, s_lowest;
+  constexpr int kParts = kSmall ? 1 : kKvCluster;
   cg::cluster_group cluster = cg::this_cluster();
-  const int rank = (int)cluster.block_rank(), b = threadIdx.x;
+  const int rank = kSmall ? 0 : (int)cluster.block_rank(), b = threadIdx.x, lane = b & 31;
+  int* refs = kSmall ? held_by : v.page_tmp;
+  const int per = (v.n_pages + kParts - 1) / kParts, p_lo = rank * per, p_hi = min(v.n_pages, p_lo + per);
+  auto barrier = [&] {
+    if (kSmall) __syncthreads(); else cluster.sync();
+  };
   pdl_wait();
   // every CTA reads and judges all places
   const bool mine = b < v.max_seqs;
-  int tokens = 0, news = 0;
+  int tokens = 0, news = 0, old = 0;
   bool bad = false;
   s_src[b] = b;
-  s_old[b] = mine ? kv_pages_of(v.lens[b], v.page_shift) : 0;
+  if (mine) old = kv_pages_of(v.lens[b], v.page_shift);
   if (mine && load) {
     tokens = len[b];
     news = n_new ? n_new[b] : 0;
     bad = tokens < 0 || tokens > v.max_pages << v.page_shift || news < 0 || news > v.max_new || news > tokens;
   } else if (mine) {
     const int s = src ? src[b] : b;
+    const int want = len ? len[b] : -1;
     bad = s < -1 || s >= v.max_seqs;
     const int held = bad || s < 0 ? 0 : v.lens[s];
-    const int want = len ? len[b] : -1;
     tokens = want == -1 || s < 0 ? held : want;
     bad = bad || tokens < 0 || tokens > held;
-    s_src[b] = s;
+    s_src[b] = s < 0 ? 0 : s;
   }
-  s_pages[b] = bad ? 0 : kv_pages_of(tokens, v.page_shift);
-  if (b == 0) s_bad = s_free = 0, s_first = v.n_pages;
-  if (__syncthreads_or(bad)) {               // the same in every CTA
+  const int pages = bad ? 0 : kv_pages_of(tokens, v.page_shift);
+  s_pages[b] = pages;
+  s_all[b] = max(pages, old);
+  s_step[b] = news > 0 ? (tokens - news) >> v.page_shift : 0x7fffffff;
+  if (b == 0) s_bad = s_free = 0, s_lowest = v.n_pages;
+  for (int p = p_lo + b; p < p_hi; p += kKvPlanThreads) refs[p] = 0;
+  unsigned long long sums;
+  s_first[b] = (int)block_scan((unsigned long long)((s_all[b] + 31) / 32) | (unsigned long long)bad << 40, &sums);
+  const int chunks = (int)(sums & 0xffffffffffULL);
+  if (sums >> 40) {                          // the same in every CTA
     if (rank == 0 && b == 0) kv_refuse(v, LIF_ERR_INVALID_ARG);
     return;
   }
-  const int per = (v.n_pages + kKvCluster - 1) / kKvCluster;
-  const int p_lo = rank * per, p_hi = min(v.n_pages, p_lo + per);
-  for (int p = p_lo + b; p < p_hi; p += kKvPlanThreads) v.page_tmp[p] = 0;
-  cluster.sync();                            // page_tmp is zero; lens and s_* are read and written
-  for (int r = rank; r < v.max_seqs; r += kKvCluster) {
-    const int32_t* row = from + (size_t)(s_src[r] < 0 ? 0 : s_src[r]) * v.max_pages;
-    for (int j = b; j < s_pages[r]; j += kKvPlanThreads) {
-      int page = row[j];
-      if (page < 0 || page >= v.n_pages) {
-        page = 0;
-        s_bad = 1;
-      }
-      v.table_tmp[(size_t)r * v.max_pages + j] = page;
-      atomicAdd(v.page_tmp + page, 1);
+  barrier();                                 // references are zero, lengths read, s_first written
+  const int c0 = rank * (kKvPlanThreads / 32) + (b >> 5), step = kParts * (kKvPlanThreads / 32);
+  auto entry = [&](int c, int* row, int* j) {
+    *row = row_of_chunk(s_first, v.max_seqs, c);
+    *j = (c - s_first[*row]) * 32 + lane;
+    int page = -1;
+    if (*j < s_pages[*row]) {
+      page = from[(size_t)s_src[*row] * v.max_pages + *j];
+      if (page < 0 || page >= v.n_pages) page = -2;
+    }
+    return page;
+  };
+  auto count = [&](int page) {
+    if (page == -2) s_bad = 1;
+    if (page >= 0) atomicAdd(refs + page, 1);
+  };
+  int row[kEarlyChunks], col[kEarlyChunks], early[kEarlyChunks];
+#pragma unroll
+  for (int i = 0; i < kEarlyChunks; ++i) {
+    early[i] = -1;
+    if (c0 + i * step < chunks) early[i] = entry(c0 + i * step, &row[i], &col[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < kEarlyChunks; ++i) count(early[i]);
+  for (int c = c0 + kEarlyChunks * step; c < chunks; c += step) {
+    int r, j;
+    const int page = entry(c, &r, &j);
+    if (page >= 0) v.table_tmp[(size_t)r * v.max_pages + j] = page;
+    count(page);
+  }
+  barrier();                                 // references are counted
+  if (load && n_new) {
+    // pages that the step's tokens lie in belong to one entry only
+    auto alone = [&](int page, int r, int j) {
+      if (page >= 0 && j >= s_step[r] && (kSmall ? refs[page] : __ldcg(refs + page)) != 1) s_bad = 1;
+    };
+#pragma unroll
+    for (int i = 0; i < kEarlyChunks; ++i)
+      if (c0 + i * step < chunks) alone(early[i], row[i], col[i]);
+    for (int c = c0 + kEarlyChunks * step; c < chunks; c += step) {
+      const int r = row_of_chunk(s_first, v.max_seqs, c), j = (c - s_first[r]) * 32 + lane;
+      if (j < s_pages[r]) alone(v.table_tmp[(size_t)r * v.max_pages + j], r, j);
     }
   }
-  cluster.sync();                            // references are counted
-  if (load && mine && news > 0 && b % kKvCluster == rank) {
-    // pages that the step's tokens lie in belong to one entry only
-    for (int j = (tokens - news) >> v.page_shift; j < s_pages[b]; ++j)
-      if (__ldcg(v.page_tmp + __ldcg(v.table_tmp + (size_t)b * v.max_pages + j)) != 1) s_bad = 1;
-  }
-  cluster.sync();
-  bool any = false;
-  for (int c = 0; c < kKvCluster; ++c) any = any || *cluster.map_shared_rank(&s_bad, c) != 0;
+  barrier();
+  bool any = s_bad != 0;
+  if (!kSmall)
+    for (int c = 0; c < kKvCluster; ++c) any = any || *cluster.map_shared_rank(&s_bad, c) != 0;
   if (any) {                                 // the same in every CTA
     if (rank == 0 && b == 0) kv_refuse(v, LIF_ERR_INVALID_ARG);
-    cluster.sync();                          // nobody leaves while its flag may be read
+    barrier();                               // nobody leaves while its flag may be read
     return;
   }
-  for (int r = rank; r < v.max_seqs; r += kKvCluster) {
-    const int n = s_pages[r], m = max(n, s_old[r]);
-    for (int j = b; j < m; j += kKvPlanThreads)
-      v.table[(size_t)r * v.max_pages + j] = j < n ? v.table_tmp[(size_t)r * v.max_pages + j] : -1;
+#pragma unroll
+  for (int i = 0; i < kEarlyChunks; ++i)
+    if (c0 + i * step < chunks && col[i] < s_all[row[i]]) v.table[(size_t)row[i] * v.max_pages + col[i]] = early[i];
+  for (int c = c0 + kEarlyChunks * step; c < chunks; c += step) {
+    const int r = row_of_chunk(s_first, v.max_seqs, c), j = (c - s_first[r]) * 32 + lane;
+    if (j < s_all[r]) v.table[(size_t)r * v.max_pages + j] = j < s_pages[r] ? v.table_tmp[(size_t)r * v.max_pages + j] : -1;
   }
   int free_here = 0, lowest = v.n_pages;
   for (int p = p_lo + b; p < p_hi; p += kKvPlanThreads) {
-    const int r = __ldcg(v.page_tmp + p);
+    const int r = kSmall ? refs[p] : __ldcg(refs + p);
     v.refs[p] = r;
     if (r == 0) {
       ++free_here;
@@ -315,18 +378,19 @@ kv_arrange_kernel(KvView v, const int32_t* from, const int32_t* src, const int32
   }
   free_here = __reduce_add_sync(~0u, free_here);
   lowest = __reduce_min_sync(~0u, lowest);
-  if ((b & 31) == 0) {
+  if (lane == 0) {
     atomicAdd(&s_free, free_here);
-    atomicMin(&s_first, lowest);
+    atomicMin(&s_lowest, lowest);
   }
-  cluster.sync();
+  barrier();
   if (rank == 0) {
     if (b == 0) {
-      int n = 0, p = v.n_pages;
-      for (int c = 0; c < kKvCluster; ++c) {
-        n += *cluster.map_shared_rank(&s_free, c);
-        p = min(p, *cluster.map_shared_rank(&s_first, c));
-      }
+      int n = s_free, p = s_lowest;
+      if (!kSmall)
+        for (int c = 1; c < kKvCluster; ++c) {
+          n += *cluster.map_shared_rank(&s_free, c);
+          p = min(p, *cluster.map_shared_rank(&s_lowest, c));
+        }
       v.counts[LIF_KV_CNT_FREE] = n;
       v.counts[KV_FREE_FROM] = p;
     }
@@ -336,7 +400,96 @@ kv_arrange_kernel(KvView v, const int32_t* from, const int32_t* src, const int32
     }
     kv_plan(v, tokens, news);
   }
-  cluster.sync();
+  if (!kSmall) cluster.sync();
+}
+
+// Tables that one CTA handles: refs and their ids in 16 bits in its shared memory.
+constexpr int kSmallPages = 40000, kSmallTable = 1 << 16;
+
+__global__ void __launch_bounds__(kKvPlanThreads)
+kv_compact_small_kernel(KvView v) {
+  extern __shared__ unsigned short ids[];    // [n_pages] new ids of those that move, [n_pages / 2] from, [n_pages / 2] to
+  __shared__ int s_first[kKvPlanThreads], s_pages[kKvPlanThreads];
+  __shared__ int s_moves;
+  pdl_wait();
+  const int b = threadIdx.x, lane = b & 31;
+  unsigned short *from = ids + v.n_pages, *to = from + v.n_pages / 2;
+  auto refs_of = [&](int p) {                // four pages' flags
+    unsigned mask = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (p + i < v.n_pages && v.refs[p + i] > 0) mask |= 1u << i;
+    return mask;
+  };
+  unsigned held = refs_of(4 * b);
+  const int used = v.n_pages - v.counts[LIF_KV_CNT_FREE];
+  s_pages[b] = b < v.max_seqs ? kv_pages_of(v.lens[b], v.page_shift) : 0;
+  if (b == 0) s_moves = 0;
+  unsigned long long chunks64;
+  s_first[b] = (int)block_scan((s_pages[b] + 31) / 32, &chunks64);
+  const int chunks = (int)chunks64;
+  __syncthreads();
+  // the table's entries travel while the lists are made
+  const int c0 = b >> 5, step = kKvPlanThreads / 32;
+  int32_t* at[kEarlyChunks];
+  int early[kEarlyChunks];
+  auto place = [&](int c) -> int32_t* {
+    const int r = row_of_chunk(s_first, v.max_seqs, c), j = (c - s_first[r]) * 32 + lane;
+    return j < s_pages[r] ? v.table + (size_t)r * v.max_pages + j : nullptr;
+  };
+#pragma unroll
+  for (int i = 0; i < kEarlyChunks; ++i) {
+    at[i] = c0 + i * step < chunks ? place(c0 + i * step) : nullptr;
+    early[i] = at[i] ? *at[i] : 0;
+  }
+  // holes below `used`, ascending, and used pages from there on, descending: equally many
+  int before = 0;
+  for (int p0 = 0;;) {
+    unsigned long long here;
+    int below = before + (int)block_scan(__popc(held), &here), moves = 0;
+    const int p = p0 + 4 * b;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int u = held >> i & 1;
+      if (p + i < v.n_pages) {
+        if (!u && p + i < used) to[p + i - below] = (unsigned short)(p + i);
+        if (u && p + i >= used) {
+          from[used - 1 - below] = (unsigned short)(p + i);
+          ++moves;
+        }
+      }
+      below += u;
+    }
+    moves = __reduce_add_sync(~0u, moves);
+    if (lane == 0 && moves) atomicAdd(&s_moves, moves);
+    before += (int)here;
+    p0 += 4 * kKvPlanThreads;
+    if (p0 >= v.n_pages) break;
+    held = refs_of(p0 + 4 * b);
+  }
+  __syncthreads();
+  const int moves = s_moves;
+  for (int j = b; j < moves; j += kKvPlanThreads) {
+    const int s = from[j], d = to[j];
+    ids[s] = (unsigned short)d;
+    v.list_a[j] = s;
+    v.list_b[j] = d;
+    v.copy_tokens[j] = 1 << v.page_shift;
+    v.refs[d] = v.refs[s];
+    v.refs[s] = 0;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kEarlyChunks; ++i)
+    if (at[i] && early[i] >= used) *at[i] = ids[early[i]];
+  for (int c = c0 + kEarlyChunks * step; c < chunks; c += step) {
+    int32_t* e = place(c);
+    if (e && *e >= used) *e = ids[*e];
+  }
+  if (b == 0) {
+    v.counts[LIF_KV_CNT_COPIES] = moves;
+    v.counts[KV_FREE_FROM] = used;
+  }
 }
 
 __global__ void __cluster_dims__(kKvCluster, 1, 1) __launch_bounds__(kKvPlanThreads)
@@ -452,6 +605,16 @@ kv_copy_pages_kernel(KvView v, uint4* pages, int n_layers, int head_bytes, int u
     for (int k = 0; k < kCopyUnit / 512; ++k)
       if ((k * 32 + lane) * 16 < bytes) d[k * 32 + lane] = x[k];
   }
+}
+
+bool small_tables(const KvView& v) { return v.n_pages <= kSmallPages && (long long)v.max_seqs * v.max_pages <= kSmallTable; }
+
+cudaError_t launch_arrange(const lif_kv* kv, const int32_t* from, const int32_t* src, const int32_t* len, const int32_t* n_new,
+                           int load, cudaStream_t st) {
+  if (small_tables(kv->v))
+    return launch_k(kv_arrange_kernel<true>, dim3(1), dim3(kKvPlanThreads), (size_t)kv->v.n_pages * 4, st, 1, kv->v, from, src, len,
+                    n_new, load);
+  return launch_k(kv_arrange_kernel<false>, dim3(kKvCluster), dim3(kKvPlanThreads), 0, st, 1, kv->v, from, src, len, n_new, load);
 }
 
 cudaError_t launch_copies(const lif_kv* kv, cudaStream_t st) {
@@ -625,6 +788,9 @@ lif_status lif_kv_create(const lif_kv_desc* desc, lif_kv** out) {
             cudaDeviceGetAttribute(&kv->n_sm, cudaDevAttrMultiProcessorCount, kv->device) == cudaSuccess &&
             kv_attention_configure(kv, &per_sm) && per_sm > 0;
   v.ctas = ok ? kv->n_sm * per_sm < kKvMaxCtas ? kv->n_sm * per_sm : kKvMaxCtas : 0;
+  ok = ok && cudaFuncSetAttribute(kv_reserve_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kReserveListMost * 4) == cudaSuccess &&
+       cudaFuncSetAttribute(kv_arrange_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallPages * 4) == cudaSuccess &&
+       cudaFuncSetAttribute(kv_compact_small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallPages * 4 + 4) == cudaSuccess;
   ok = ok && (pairs == 0 || cudaMemcpy(base + w.turns, turns, (size_t)pairs * 8, cudaMemcpyHostToDevice) == cudaSuccess);
   ok = ok && lif_kv_reset(kv, nullptr) == LIF_OK && cudaDeviceSynchronize() == cudaSuccess;
   if (!ok) {
@@ -660,7 +826,7 @@ lif_status lif_kv_reserve(lif_kv* kv, const int32_t* dev_n_new, void* stream) {
   const lif_status s = enter(kv);
   if (s != LIF_OK) return s;
   cudaStream_t st = (cudaStream_t)stream;
-  cudaError_t e = launch_k(kv_reserve_kernel, dim3(1), dim3(kKvPlanThreads), 0, st, 1, kv->v, dev_n_new);
+  cudaError_t e = launch_k(kv_reserve_kernel, dim3(1), dim3(kKvPlanThreads), (size_t)reserve_list(kv->v) * 4, st, 1, kv->v, dev_n_new);
   if (e == cudaSuccess) e = launch_copies(kv, st);
   return done(e);
 }
@@ -670,8 +836,7 @@ lif_status lif_kv_fork(lif_kv* kv, const int32_t* dev_src, const int32_t* dev_le
   if (!aligned(dev_src, 4) || !aligned(dev_len, 4)) return LIF_ERR_ALIGNMENT;
   const lif_status s = enter(kv);
   if (s != LIF_OK) return s;
-  return done(launch_k(kv_arrange_kernel, dim3(kKvCluster), dim3(kKvPlanThreads), 0, (cudaStream_t)stream, 1, kv->v,
-                       (const int32_t*)kv->v.table, dev_src, dev_len, (const int32_t*)nullptr, 0));
+  return done(launch_arrange(kv, kv->v.table, dev_src, dev_len, nullptr, 0, (cudaStream_t)stream));
 }
 
 lif_status lif_kv_load(lif_kv* kv, const int32_t* dev_lens, const int32_t* dev_table, const int32_t* dev_n_new,
@@ -680,15 +845,16 @@ lif_status lif_kv_load(lif_kv* kv, const int32_t* dev_lens, const int32_t* dev_t
   if (!aligned(dev_lens, 4) || !aligned(dev_table, 4) || !aligned(dev_n_new, 4)) return LIF_ERR_ALIGNMENT;
   const lif_status s = enter(kv);
   if (s != LIF_OK) return s;
-  return done(launch_k(kv_arrange_kernel, dim3(kKvCluster), dim3(kKvPlanThreads), 0, (cudaStream_t)stream, 1, kv->v,
-                       dev_table, (const int32_t*)nullptr, dev_lens, dev_n_new, 1));
+  return done(launch_arrange(kv, dev_table, nullptr, dev_lens, dev_n_new, 1, (cudaStream_t)stream));
 }
 
 lif_status lif_kv_compact(lif_kv* kv, void* stream) {
   const lif_status s = enter(kv);
   if (s != LIF_OK) return s;
   cudaStream_t st = (cudaStream_t)stream;
-  cudaError_t e = launch_k(kv_compact_kernel, dim3(kKvCluster), dim3(kKvPlanThreads), 0, st, 1, kv->v);
+  cudaError_t e = small_tables(kv->v)
+                      ? launch_k(kv_compact_small_kernel, dim3(1), dim3(kKvPlanThreads), (size_t)kv->v.n_pages * 4 + 4, st, 1, kv->v)
+                      : launch_k(kv_compact_kernel, dim3(kKvCluster), dim3(kKvPlanThreads), 0, st, 1, kv->v);
   if (e == cudaSuccess) e = launch_copies(kv, st);
   return done(e);
 }

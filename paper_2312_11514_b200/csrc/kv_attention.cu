@@ -34,7 +34,7 @@ namespace lif {
 namespace {
 
 struct AttendArgs {
-  const void* q;
+  const void *q, *pages;       // pages: this layer's
   void* out;
   float scale_log2;            // scale * log2(e): weights are powers of two
   int layer;
@@ -82,13 +82,21 @@ __device__ __forceinline__ void tensor_g2s(uint32_t to, const CUtensorMap* map, 
       : "memory");
 }
 
-// Byte where 16-byte piece c0 + b (c0 even and known, b 0 or 1) of row r lies in a tile of 64 rows of D
-// elements: 64 columns after 64, the rest behind them; within 128 (64, 32) bytes of a row
-// the pieces are permuted by the row as the tensor map's swizzle does it.
+// Byte where 16-byte piece c of row r lies in a tile of 64 rows of D elements: 64 columns after 64, the rest
+// behind them; within 128 (64) bytes of a row the pieces are permuted by the row as the tensor map's swizzle
+// does it.  Rows of 80 elements lie as they are: only rows r and r + 4 meet in a bank, and one copy
+// a page and operand in place of two, the second 32 bytes wide, took 16.5 us where two took LINEAR_FIGURE.
+template <int D>
+__device__ __forceinline__ uint32_t piece(int r, int c) {
+  if (D == 80) return r * 160 + c * 16;
+  if (c < D / 64 * 8) return (c / 8) * 8192 + r * 128 + (((c & 7) ^ (r & 7)) << 4);
+  return D / 64 * 8192 + r * 64 + (((c & 3) ^ (r >> 1 & 3)) << 4);
+}
+// the same for piece c0 + b, c0 even and known, b 0 or 1
 template <int D>
 __device__ __forceinline__ uint32_t piece(int r, int c0, int b) {
-  if (c0 / 8 < D / 64) return (c0 / 8) * 8192 + r * 128 + (((c0 & 7) ^ (b ^ (r & 7))) << 4);
-  if (D % 64 == 16) return D / 64 * 8192 + r * 32 + ((b ^ (r >> 2 & 1)) << 4);
+  if (D == 80) return r * 160 + b * 16 + c0 * 16;
+  if (c0 < D / 64 * 8) return (c0 / 8) * 8192 + r * 128 + (((c0 & 7) ^ (b ^ (r & 7))) << 4);
   return D / 64 * 8192 + r * 64 + (((c0 & 3) ^ (b ^ (r >> 1 & 3))) << 4);
 }
 
@@ -105,7 +113,7 @@ struct Shape {
   static constexpr int kQuerySlot = kRows * kPitch;                      // two: the next head's arrive meanwhile
   static constexpr int kTiles = D / 8;                                   // 8-column tiles of the output
   // the sum over the WK warps of a row: so many of a warp's rows at a time
-  static constexpr int kSumRows = D < 128 || kWarps > 4 ? 4 : 2, kSumPitch = D + 8;
+  static constexpr int kSumRows = WR > 1 || D == 96 ? 4 : D < 96 ? 8 : 2, kSumPitch = D + 8;
   static constexpr int kScratch = WK > 1 ? kWarps * kSumRows * kSumPitch * 4 : 0;
   static constexpr int kMaxStages = 6;
   static constexpr int kFixed = 2 * kQuerySlot + kScratch + kRows * WK * 8 + kMaxStages * (int)sizeof(StageInfo) + 256;
@@ -155,7 +163,8 @@ template <typename T, int D, int WR, int WK>
 __device__ __forceinline__ void feed(const KvMaps& maps, const KvView& V, const AttendArgs& a, unsigned char* ring,
                                      unsigned char* queries, StageInfo* info, Barriers* bars, int4 plan, int4 step) {
   using S = Shape<D, WR, WK>;
-  constexpr int kChunks = (D + 63) / 64;
+  constexpr bool kLinear = D == 80;                  // a page's rows of a head as they are
+  constexpr int kChunks = kLinear ? 1 : (D + 63) / 64;
   const int lane = threadIdx.x & 31;
   const int page_tokens = 1 << V.page_shift, box = min(page_tokens, kKvTile);
   const int pages_a_tile = kKvTile / box;
@@ -223,9 +232,13 @@ __device__ __forceinline__ void feed(const KvMaps& maps, const KvView& V, const 
     for (int x0 = 0; x0 < n_pages * 2 * kChunks; x0 += 32) {
       const int x = x0 + lane, p = x / (2 * kChunks), what = x / kChunks & 1, chunk = x % kChunks;
       const int page = __shfl_sync(~0u, held, j0 - held_from + p & 31);
-      if (p < n_pages) {
+      if (kLinear && p < n_pages) {
+        const int64_t head = ((int64_t)page * 2 + what) * V.n_kv_heads + at.head;
+        bulk_g2s(ring + stage * S::kStage + what * S::kTileBytes + p * box * D * 2,
+                 reinterpret_cast<const T*>(a.pages) + ((head << V.page_shift) + (k0 & (page_tokens - 1))) * D, box * D * 2, bar);
+      } else if (p < n_pages) {
         const bool full = D % 64 == 0 || chunk < D / 64;
-        tensor_g2s(keys + what * S::kTileBytes + chunk * 8192 + p * box * (full ? 128 : D % 64 * 2),
+        tensor_g2s(keys + what * S::kTileBytes + chunk * 8192 + p * box * (full ? 128 : 64),
                    full ? &maps.wide : &maps.rest, chunk * 64, k0 & (page_tokens - 1), what * V.n_kv_heads + at.head, page,
                    a.layer, bar);
       }
@@ -289,7 +302,7 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
 
   if (threadIdx.x == 32) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.wide) : "memory");
-    if (D % 64) asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.rest) : "memory");
+    if (D == 96) asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.rest) : "memory");
   }
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::kStages; ++i) {
@@ -403,9 +416,7 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
             const int r = wk * kKeys + k, key = first + k;
             const bool none = key < some || key >= at.tokens;
             if (c >= kPieces || !(none || differ)) continue;
-            uint4* v = reinterpret_cast<uint4*>(smem + (values - ring) + (c / 8 < D / 64 ? (c / 8) * 8192 + r * 128 + ((c & 7) ^ (r & 7)) * 16
-                                                                         : D % 64 == 16 ? D / 64 * 8192 + r * 32 + ((c & 1) ^ (r >> 2 & 1)) * 16
-                                                                                        : D / 64 * 8192 + r * 64 + ((c & 3) ^ (r >> 1 & 3)) * 16));
+            uint4* v = reinterpret_cast<uint4*>(smem + (values - ring) + piece<D>(r, c));
             if (none) {
               *v = make_uint4(0, 0, 0, 0);
             } else {
@@ -442,7 +453,9 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           top[h] = fmaxf(top[h], __shfl_xor_sync(~0u, top[h], 1));
-          top[h] = fmaxf(fmaxf(top[h], __shfl_xor_sync(~0u, top[h], 2)), m[h]);
+          top[h] = fmaxf(top[h], __shfl_xor_sync(~0u, top[h], 2));
+          // (each row by itself: what a row gets must not depend on the others, which may not be there)
+          if (!(top[h] > m[h] + kSlack)) top[h] = m[h];
           shrink[h] = power(m[h] - (top[h] == -INFINITY ? 0.f : top[h]));
           m[h] = top[h];
           sum[h] *= shrink[h];
@@ -780,10 +793,8 @@ int kv_row_tiles(const lif_kv_desc& d) {
 }
 
 bool kv_attention_configure(lif_kv* kv, int* ctas_per_sm) {
-  const int rest = kv->desc.head_dim % 64;
   if (!encode_map(&kv->maps.wide, kv->desc, 64, CU_TENSOR_MAP_SWIZZLE_128B)) return false;
-  if (rest && !encode_map(&kv->maps.rest, kv->desc, rest, rest == 16 ? CU_TENSOR_MAP_SWIZZLE_32B : CU_TENSOR_MAP_SWIZZLE_64B))
-    return false;
+  if (kv->desc.head_dim == 96 && !encode_map(&kv->maps.rest, kv->desc, 32, CU_TENSOR_MAP_SWIZZLE_64B)) return false;
   return with_kernel(kv, [&](auto kernel, auto, int threads, int smem, auto) {
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(ctas_per_sm, kernel, threads, smem);
@@ -792,11 +803,13 @@ bool kv_attention_configure(lif_kv* kv, int* ctas_per_sm) {
 }
 
 cudaError_t launch_kv_attention(const lif_kv* kv, int layer, const void* q, void* out, cudaStream_t st) {
+  const lif_kv_desc& d = kv->desc;
   AttendArgs a;
   a.q = q;
   a.out = out;
   a.scale_log2 = kv->scale * 1.4426950408889634f;
   a.layer = layer;
+  a.pages = (const char*)d.dev_pages + (size_t)layer * d.n_pages * kv_page_elems(d) * 2;
   return with_kernel(kv, [&](auto kernel, auto join, int threads, int smem, auto* type) {
     cudaError_t e = launch_k2(kernel, dim3(kv->v.ctas), dim3(threads), smem, st, 1, 1, kv->maps, kv->v, a);
     if (e == cudaSuccess) e = launch_k2(join, dim3(kv->n_sm), dim3(kJoinThreads), 0, st, 1, 1, kv->v, (decltype(type))out);

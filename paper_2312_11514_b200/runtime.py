@@ -172,6 +172,9 @@ class KvCache:
         self.dtype, self.max_seqs, self.max_new, self.norm = dtype, max_seqs, max_new, norm
         self.n_heads, self.n_kv_heads, self.head_dim, self.n_layers = n_heads, n_kv_heads, head_dim, n_layers
         self.max_pages = n_pages if max_pages is None else max_pages
+        self._index = self.device.index if self.device.index is not None else torch.cuda.current_device()
+        self._queries, self._keys = (max_seqs, max_new, n_heads, head_dim), (max_seqs, max_new, n_kv_heads, head_dim)
+        self._places, self._table = (max_seqs,), (max_seqs, self.max_pages)
         shape = dict(n_layers=n_layers, n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim,
                      dtype=self._TYPES[dtype], page_tokens=page_tokens, n_pages=n_pages, max_seqs=max_seqs,
                      max_pages=self.max_pages, max_new=max_new, window=window, scale=scale or 0.0, norm=norm,
@@ -205,7 +208,8 @@ class KvCache:
     _GUARD = 0x7B
 
     def _expect(self, name, t, shape, dtype=None, contiguous=True):
-        if t.device != self.device or t.dtype != (dtype or self.dtype) or tuple(t.shape) != tuple(shape) or \
+        # (a decode step makes several calls a layer: what is compared here is what torch answers fastest)
+        if t.get_device() != self._index or t.dtype is not (dtype or self.dtype) or t.shape != shape or \
                 (contiguous and not t.is_contiguous()):
             raise ValueError(f"KvCache: {name} is {tuple(t.shape)} {t.dtype} on {t.device}"
                              f"{'' if t.is_contiguous() else ', not contiguous'}; expected {tuple(shape)} "
@@ -213,21 +217,22 @@ class KvCache:
 
     def _ints(self, name, t, shape=None):
         if t is not None:
-            self._expect(name, t, shape or (self.max_seqs,), torch.int32)
+            self._expect(name, t, shape or self._places, torch.int32)
         return t
 
     def _on(self, stream):
-        return torch.cuda.current_stream(self.device) if stream is None else stream
+        return torch._C._cuda_getCurrentRawStream(self._index) if stream is None else stream
 
-    def _rows(self, name, t, heads):
-        self._expect(name, t, (self.max_seqs, self.max_new, heads, self.head_dim), contiguous=False)
+    def _rows(self, name, t, shape):
+        self._expect(name, t, shape, contiguous=False)
+        places, tokens, step, element = t.stride()
+        many, several = self.max_seqs > 1, self.max_new > 1
         # places lie max_new tokens apart
-        if t.stride(3) != 1 or (self.max_seqs > 1 and self.max_new > 1 and t.stride(0) != self.max_new * t.stride(1)):
+        if element != 1 or (many and several and places != self.max_new * tokens):
             raise ValueError(f"KvCache: {name} has strides {t.stride()}; places have to lie max_new tokens apart, "
                              f"a head's elements beside each other")
         # (torch leaves the stride of a dimension of one element undefined)
-        step = t.stride(1) if self.max_new > 1 else t.stride(0) if self.max_seqs > 1 else 0
-        return B.KvRows(t.data_ptr(), step, t.stride(2) if heads > 1 else 0)
+        return B.KvRows(t.data_ptr(), tokens if several else places if many else 0, step if shape[2] > 1 else 0)
 
     def reserve(self, n_new: torch.Tensor, stream=None) -> None:
         B.lif_kv_reserve(self.handle, self._ints("n_new", n_new), self._on(stream))
@@ -238,27 +243,25 @@ class KvCache:
         projection's output are fine.  ``norms``: query weight, query bias, key weight, key bias.
         Returns the normed and rotated queries (rows of tokens that are not there are not written)."""
         if q_out is None:
-            q_out = torch.empty(self.max_seqs, self.max_new, self.n_heads, self.head_dim, dtype=self.dtype,
-                                device=self.device)
+            q_out = torch.empty(self._queries, dtype=self.dtype, device=self.device)
         else:
-            self._expect("q_out", q_out, (self.max_seqs, self.max_new, self.n_heads, self.head_dim))
+            self._expect("q_out", q_out, self._queries)
         weights = None
         if self.norm != B.NORM_NONE and norms is not None:
             for t in norms:
                 if t is not None:
                     self._expect("norm weight", t, (self.head_dim,))
             weights = B.KvNorms(*[None if t is None else t.data_ptr() for t in norms])
-        B.lif_kv_append(self.handle, layer, self._rows("q", q, self.n_heads), self._rows("k", k, self.n_kv_heads),
-                        self._rows("v", v, self.n_kv_heads), weights, q_out, self._on(stream))
+        B.lif_kv_append(self.handle, layer, self._rows("q", q, self._queries), self._rows("k", k, self._keys),
+                        self._rows("v", v, self._keys), weights, q_out, self._on(stream))
         return q_out
 
     def attention(self, layer: int, q: torch.Tensor, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-        shape = (self.max_seqs, self.max_new, self.n_heads, self.head_dim)
-        self._expect("q", q, shape)
+        self._expect("q", q, self._queries)
         if out is None:
             out = torch.empty_like(q)
         else:
-            self._expect("out", out, shape)
+            self._expect("out", out, self._queries)
         B.lif_kv_attention(self.handle, layer, q, out, self._on(stream))
         return out
 
@@ -266,7 +269,7 @@ class KvCache:
         B.lif_kv_fork(self.handle, self._ints("src", src), self._ints("length", length), self._on(stream))
 
     def load(self, lens: torch.Tensor, table: torch.Tensor, n_new: Optional[torch.Tensor] = None, stream=None) -> None:
-        B.lif_kv_load(self.handle, self._ints("lens", lens), self._ints("table", table, (self.max_seqs, self.max_pages)),
+        B.lif_kv_load(self.handle, self._ints("lens", lens), self._ints("table", table, self._table),
                       self._ints("n_new", n_new), self._on(stream))
 
     def compact(self, stream=None) -> None:
