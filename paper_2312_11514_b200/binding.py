@@ -162,7 +162,7 @@ def lib() -> C.CDLL:
         "lif_kv_get_state": [vp, C.POINTER(KvState)],
         "lif_kv_reset": [vp, vp],
         "lif_kv_reserve": [vp, vp, vp],
-        "lif_kv_append": [vp, i32, C.POINTER(KvRows), C.POINTER(KvRows), C.POINTER(KvRows), C.POINTER(KvNorms), vp, vp],
+        "lif_kv_append": [vp, i32, vp, vp, vp, vp, vp, vp],
         "lif_kv_attention": [vp, i32, vp, vp, vp],
         "lif_kv_fork": [vp, vp, vp, vp],
         "lif_kv_load": [vp, vp, vp, vp, vp],

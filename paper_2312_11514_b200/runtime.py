@@ -5,6 +5,7 @@ from __future__ import annotations
 
 import ctypes as C
 import math
+import struct
 from typing import Dict, List, Optional, Sequence
 
 import torch
@@ -148,6 +149,10 @@ def rope_frequencies(dims: int, base: float = 10000.0, scaling: str = "none", fa
     return out
 
 
+# lif_kv_rows and lif_kv_norms as bytes: a quarter of the time that ctypes takes to fill a structure
+_ROWS, _NORMS = struct.Struct("=3q").pack, struct.Struct("=4q").pack
+
+
 class KvCache:
     """A paged key-value cache for the attention between the FFN layers (include/lif_kv.h): owns its
     workspace (and the pool, unless ``pages`` is given) and the handle.  Tensors are checked here for
@@ -174,7 +179,8 @@ class KvCache:
         self.max_pages = n_pages if max_pages is None else max_pages
         self._index = self.device.index if self.device.index is not None else torch.cuda.current_device()
         self._queries, self._keys = (max_seqs, max_new, n_heads, head_dim), (max_seqs, max_new, n_kv_heads, head_dim)
-        self._places, self._table = (max_seqs,), (max_seqs, self.max_pages)
+        self._places, self._table, self._head = (max_seqs,), (max_seqs, self.max_pages), (head_dim,)
+        self._lib = B.lib()
         shape = dict(n_layers=n_layers, n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim,
                      dtype=self._TYPES[dtype], page_tokens=page_tokens, n_pages=n_pages, max_seqs=max_seqs,
                      max_pages=self.max_pages, max_new=max_new, window=window, scale=scale or 0.0, norm=norm,
@@ -224,15 +230,16 @@ class KvCache:
         return torch._C._cuda_getCurrentRawStream(self._index) if stream is None else stream
 
     def _rows(self, name, t, shape):
-        self._expect(name, t, shape, contiguous=False)
+        if t.get_device() != self._index or t.dtype is not self.dtype or t.shape != shape:
+            self._expect(name, t, shape, contiguous=False)
         places, tokens, step, element = t.stride()
         many, several = self.max_seqs > 1, self.max_new > 1
         # places lie max_new tokens apart
         if element != 1 or (many and several and places != self.max_new * tokens):
             raise ValueError(f"KvCache: {name} has strides {t.stride()}; places have to lie max_new tokens apart, "
                              f"a head's elements beside each other")
-        # (torch leaves the stride of a dimension of one element undefined)
-        return B.KvRows(t.data_ptr(), tokens if several else places if many else 0, step if shape[2] > 1 else 0)
+        # a KvRows (torch leaves the stride of a dimension of one element undefined)
+        return _ROWS(t.data_ptr(), tokens if several else places if many else 0, step if shape[2] > 1 else 0)
 
     def reserve(self, n_new: torch.Tensor, stream=None) -> None:
         B.lif_kv_reserve(self.handle, self._ints("n_new", n_new), self._on(stream))
@@ -250,10 +257,12 @@ class KvCache:
         if self.norm != B.NORM_NONE and norms is not None:
             for t in norms:
                 if t is not None:
-                    self._expect("norm weight", t, (self.head_dim,))
-            weights = B.KvNorms(*[None if t is None else t.data_ptr() for t in norms])
-        B.lif_kv_append(self.handle, layer, self._rows("q", q, self._queries), self._rows("k", k, self._keys),
-                        self._rows("v", v, self._keys), weights, q_out, self._on(stream))
+                    self._expect("norm weight", t, self._head)
+            weights = _NORMS(*[0 if t is None else t.data_ptr() for t in norms])
+        code = self._lib.lif_kv_append(self.handle, layer, self._rows("q", q, self._queries), self._rows("k", k, self._keys),
+                                       self._rows("v", v, self._keys), weights, q_out.data_ptr(), B._stream(self._on(stream)))
+        if code:
+            raise B.LifError(code, "lif_kv_append")
         return q_out
 
     def attention(self, layer: int, q: torch.Tensor, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
@@ -262,7 +271,9 @@ class KvCache:
             out = torch.empty_like(q)
         else:
             self._expect("out", out, self._queries)
-        B.lif_kv_attention(self.handle, layer, q, out, self._on(stream))
+        code = self._lib.lif_kv_attention(self.handle, layer, q.data_ptr(), out.data_ptr(), B._stream(self._on(stream)))
+        if code:
+            raise B.LifError(code, "lif_kv_attention")
         return out
 
     def fork(self, src: Optional[torch.Tensor] = None, length: Optional[torch.Tensor] = None, stream=None) -> None:
