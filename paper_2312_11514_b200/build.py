@@ -11,7 +11,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "liblif.so")
 SOURCES = ["api.cu", "predict.cu", "gate.cu", "window.cu", "fetch.cu", "ffn.cu", "ffn_batched.cu", "exchange.cu", "store.cu", "step.cu",
-           "kv.cu", "kv_append.cu", "kv_attention.cu"]
+           "kv.cu", "kv_append.cu", "kv_attention.cu", "kv_attention_wide.cu"]
 
 
 def _nvcc() -> str:

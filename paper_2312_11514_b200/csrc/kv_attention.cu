@@ -28,33 +28,11 @@
 // Precision.  Scores, maxima, sums and outputs are fp32.  Weights are rounded to the cache's type
 // for the second product (at most half a unit in the last place of each, like the rounding of the
 // output); the sum is that of the rounded weights, so that they add up to one exactly as they are used.
-#include "kv_internal.cuh"
+#include "kv_attention.cuh"
 
 namespace lif {
 namespace {
 
-struct AttendArgs {
-  const void *q, *pages;       // pages: this layer's
-  void* out;
-  float scale_log2;            // scale * log2(e): weights are powers of two
-  int layer;
-};
-
-// What a stage of the ring holds.
-struct __align__(16) StageInfo {
-  int b, tokens, news, k0;     // place, its tokens, its new ones, first key
-  int head, row0, flags;       // key-value head, first row of the row block
-  int run;
-};
-// first tile of a piece, of the head; last tile of the head, of a piece, of the CTA; keys that not every row sees
-enum { kOpens = 1, kStarts = 2, kEnds = 4, kCloses = 8, kLast = 16, kEdge = 32 };
-
-// 2^x; results below 2^-126 are 0 (a weight that small is none in 16 bits)
-__device__ __forceinline__ float power(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ void ldm_x4(uint32_t* r, uint32_t at) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
@@ -73,33 +51,6 @@ __device__ __forceinline__ void mma(__nv_bfloat16, float* c, const uint32_t* a, 
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// a box of the pool at {column, row in the page, operand and head, page, layer}
-__device__ __forceinline__ void tensor_g2s(uint32_t to, const CUtensorMap* map, int x, int row, int head, int page,
-                                           int layer, uint64_t* bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2,%3,%4,%5,%6}], [%7];"
-      ::"r"(to), "l"(map), "r"(x), "r"(row), "r"(head), "r"(page), "r"(layer), "r"(smem_u32(bar))
-      : "memory");
-}
-
-// Byte where 16-byte piece c of row r lies in a tile of 64 rows of D elements: 64 columns after 64, the rest
-// behind them; within 128 (64) bytes of a row the pieces are permuted by the row as the tensor map's swizzle
-// does it.  Rows of 80 elements lie as they are: only rows r and r + 4 meet in a bank, and one copy
-// a page and operand in place of two, the second 32 bytes wide, took 16.5 us where two took LINEAR_FIGURE.
-template <int D>
-__device__ __forceinline__ uint32_t piece(int r, int c) {
-  if (D == 80) return r * 160 + c * 16;
-  if (c < D / 64 * 8) return (c / 8) * 8192 + r * 128 + (((c & 7) ^ (r & 7)) << 4);
-  return D / 64 * 8192 + r * 64 + (((c & 3) ^ (r >> 1 & 3)) << 4);
-}
-// the same for piece c0 + b, c0 even and known, b 0 or 1
-template <int D>
-__device__ __forceinline__ uint32_t piece(int r, int c0, int b) {
-  if (D == 80) return r * 160 + b * 16 + c0 * 16;
-  if (c0 < D / 64 * 8) return (c0 / 8) * 8192 + r * 128 + (((c0 & 7) ^ (b ^ (r & 7))) << 4);
-  return D / 64 * 8192 + r * 64 + (((c0 & 3) ^ (b ^ (r >> 1 & 3))) << 4);
-}
-
 template <int D, int WR, int WK>
 struct Shape {
   static constexpr int kRows = 16 * WR, kWarps = WR * WK;
@@ -126,34 +77,6 @@ struct Shape {
   static_assert(kStages >= 2 && kStage % 1024 == 0, "");
 };
 
-// A place in the step's work.
-struct Cursor {
-  int b, tokens, news, tiles, blocks, head, block, tile, first_tile;
-  __device__ __forceinline__ void enter(const KvView& V, int place, int n_tokens, int n_new) {
-    b = place;
-    tokens = n_tokens;
-    news = n_new;
-    tiles = kv_tiles(n_tokens, n_new, V.window);
-    blocks = kv_row_blocks(n_new, V.group, V.rows_per_block);
-    first_tile = kv_first_key(n_tokens, n_new, V.window) / kKvTile;
-  }
-  __device__ __forceinline__ void step(const KvView& V) {
-    if (++tile < tiles) return;
-    tile = 0;
-    if (++block < blocks) return;
-    block = 0;
-    if (++head < V.n_kv_heads) return;
-    head = 0;
-    for (int p = b + 1; p < V.max_seqs; ++p) {
-      const int4 s = V.seq_plan[p];
-      if (s.w > 0) {
-        enter(V, p, s.y, s.z);
-        return;
-      }
-    }
-  }
-};
-
 struct Barriers {
   uint64_t full[6], empty[6], q_empty[2], all;
 };
@@ -167,63 +90,23 @@ __device__ __forceinline__ void feed(const KvMaps& maps, const KvView& V, const 
   constexpr int kChunks = kLinear ? 1 : (D + 63) / 64;
   const int lane = threadIdx.x & 31;
   const int page_tokens = 1 << V.page_shift, box = min(page_tokens, kKvTile);
-  const int pages_a_tile = kKvTile / box;
-  const int total = step.x, share = step.z, first_tiles = step.w;
-  const int4 others = *reinterpret_cast<const int4*>(V.counts + KV_MORE_TILES);
-  const int more_tiles = others.x, more = others.y, n_more = others.z;
-  int run = blockIdx.x * (1 + more), next = 0;
-  int g = blockIdx.x * share, end = min(total, g + first_tiles);
-  Cursor at;
-  auto seek = [&](const int4& p) {                   // p: the run's entry of run_plan
-    at.enter(V, p.x, p.z, p.w);
-    const int in = g - p.y, item = in / at.tiles;
-    at.tile = in - item * at.tiles;
-    at.head = item / at.blocks;
-    at.block = item - at.head * at.blocks;
-  };
-  seek(plan);
-  int held_b = -1, held_from = 0, held = 0;          // 32 page ids of a place, one a lane
+  Walk walk(V, blockIdx.x, plan, step);
+  const Cursor& at = walk.at;
   int stage = 0, piece = 0;
   unsigned turn = 0;
-  bool lost = false, opens_run = true, last = false;
+  bool lost = false;
   int i = 0;
-  for (; !last; ++i) {
-    const int k0 = (at.first_tile + at.tile) * kKvTile, j0 = k0 >> V.page_shift;
-    const int pages = kv_pages_of(at.tokens, V.page_shift), n_pages = min(pages - j0, pages_a_tile);
-    if (at.b != held_b || (j0 & ~31) != held_from) {
-      held_b = at.b;
-      held_from = j0 & ~31;
-      held = held_from + lane < pages ? V.table[(size_t)at.b * V.max_pages + held_from + lane] : 0;
-    }
-    const bool opens = opens_run || at.tile == 0;
-    if (opens_run) {                                 // the run after this one; asked for long before it is needed
-      if (n_more && lane == 0) next = atomicAdd(V.counts + KV_TAKEN, 1);
-      opens_run = false;
-    }
-    const bool ends_run = g + 1 == end;
-    if (ends_run) {
-      next = __shfl_sync(~0u, next, 0);
-      last = next >= n_more;
-    }
+  for (; !walk.last; ++i) {
+    walk.begin(V, lane);
+    const bool opens = walk.opens;
+    const int k0 = walk.k0, n_pages = walk.n_pages;
     if (!mbar_wait(bars->empty + stage, turn ^ 1)) lost = true;
     if (opens && !mbar_wait(bars->q_empty + (piece & 1), (piece >> 1 & 1) ^ 1)) lost = true;
     if (__any_sync(~0u, lost)) break;                // (nothing of this tile is on its way)
     const int row0 = at.block * S::kRows, rows = min(S::kRows, at.news * V.group - row0);
     uint64_t* bar = bars->full + stage;
     if (lane == 0) {
-      const bool ends = at.tile + 1 == at.tiles;
-      StageInfo n;
-      n.b = at.b;
-      n.tokens = at.tokens;
-      n.news = at.news;
-      n.k0 = k0;
-      n.head = at.head;
-      n.row0 = row0;
-      n.flags = (opens ? kOpens : 0) | (at.tile == 0 ? kStarts : 0) | (ends ? kEnds : 0) |
-                (ends || ends_run ? kCloses : 0) | (last ? kLast : 0) |
-                (k0 + kKvTile > at.tokens - at.news + 1 || (V.window > 0 && k0 <= at.tokens - 1 - V.window) ? kEdge : 0);
-      n.run = run;
-      info[stage] = n;
+      info[stage] = walk.info(V);
       mbar_expect_tx(bar, n_pages * box * D * 4 + (opens ? rows * D * 2 : 0));
     }
     __syncwarp();
@@ -231,7 +114,7 @@ __device__ __forceinline__ void feed(const KvMaps& maps, const KvView& V, const 
 #pragma unroll 1
     for (int x0 = 0; x0 < n_pages * 2 * kChunks; x0 += 32) {
       const int x = x0 + lane, p = x / (2 * kChunks), what = x / kChunks & 1, chunk = x % kChunks;
-      const int page = __shfl_sync(~0u, held, j0 - held_from + p & 31);
+      const int page = __shfl_sync(~0u, walk.held, walk.j0 - walk.held_from + p & 31);
       if (kLinear && p < n_pages) {
         const int64_t head = ((int64_t)page * 2 + what) * V.n_kv_heads + at.head;
         bulk_g2s(ring + stage * S::kStage + what * S::kTileBytes + p * box * D * 2,
@@ -261,18 +144,7 @@ __device__ __forceinline__ void feed(const KvMaps& maps, const KvView& V, const 
       ++piece;
     }
     if (++stage == S::kStages) stage = 0, turn ^= 1;
-    if (!ends_run) {
-      ++g;
-      at.step(V);
-    } else if (!last) {
-      const int c = next / more, j = next - c * more;
-      run = c * (1 + more) + 1 + j;
-      plan = V.run_plan[V.ctas + next];
-      g = c * share + first_tiles + j * more_tiles;
-      end = min(min(total, c * share + share), g + more_tiles);
-      opens_run = true;
-      seek(plan);
-    }
+    walk.advance(V);
   }
   if (lost && lane == 0) flag_timeout(V.counts + LIF_KV_CNT_STATUS);
   // nobody leaves while copies are on their way
@@ -403,29 +275,21 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
             const int key = first + n * 8 + 2 * t4 + (e & 1), last_seen = upto[e >> 1];
             if (key > last_seen || last_seen - key >= reach) s[n][e] = -INFINITY;
           }
-        // keys [some, all) and [few, end) are seen by some rows, those before and behind by none
-        const int some = kv_first_key(at.tokens, at.news, V.window), all = V.window > 0 ? at.tokens - V.window : 0;
-        const int few = at.tokens - at.news + 1;
-        const bool clear = first < some || first + kKeys > at.tokens;
-        const bool differ = at.news > 1 && (first < all || first + kKeys > few);
+        const Edge edge(V, at);
+        const bool clear = edge.clear(at, first, kKeys), differ = edge.differ(at, first, kKeys);
         if (clear || differ) {
           constexpr int kPieces = D / 8, kLanes = kPieces <= 8 ? 8 : kPieces <= 16 ? 16 : 32;
           const int c = lane % kLanes;
           bool odd = false;
           for (int k = lane / kLanes; k < kKeys; k += 32 / kLanes) {
-            const int r = wk * kKeys + k, key = first + k;
-            const bool none = key < some || key >= at.tokens;
+            const int r = wk * kKeys + k;
+            const bool none = edge.none(at, first + k);
             if (c >= kPieces || !(none || differ)) continue;
             uint4* v = reinterpret_cast<uint4*>(smem + (values - ring) + piece<D>(r, c));
             if (none) {
               *v = make_uint4(0, 0, 0, 0);
             } else {
-              const uint4 bits = *v;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const uint32_t y = (&bits.x)[e], lo = Num<T>::kExponent & 0xffffu, hi = Num<T>::kExponent & 0xffff0000u;
-                odd = odd || (y & lo) == lo || (y & hi) == hi;
-              }
+              odd = odd || any_not_finite<T>(*v);
             }
           }
           one_by_one = __any_sync(~0u, odd);
@@ -433,11 +297,7 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
           if (clear) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the ring's copies come behind these stores
         }
       }
-      // Weights 2^(s - m).  m need not be the maximum, only near enough that no weight is large: it is brought
-      // up to date, and what was summed scaled down, when a score lies more than kSlack above it.  The key that
-      // set m has weight 1, so nothing gets smaller than with the maximum.  A row that has seen nothing
-      // yet has m = -inf and weights 0.
-      constexpr float kSlack = 8.f;                  // weights up to 256
+      // weights 2^(s - m); a row that has seen nothing yet has m = -inf and weights 0
       bool above = false;
       float top[2];
 #pragma unroll
@@ -535,10 +395,6 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
       const bool whole = starts && (at.flags & kEnds);
       // a piece that began before this run, or one that goes on behind it
       float* part = V.partials + (size_t)(2 * at.run + starts) * V.slot_floats;
-      auto token_head = [&](int r) {                 // row r's place in the output
-        const int t = (at.row0 + r) / V.group, h = at.row0 + r - t * V.group;
-        return (((int64_t)at.b * V.max_new + t) * V.n_heads + at.head * V.group + h) * D;
-      };
       T* out = reinterpret_cast<T*>(a.out);
       if constexpr (WK > 1) {
         // The row's WK warps lay down their outputs, a few rows at a time, and each thread sums two columns.  The
@@ -584,7 +440,7 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
               sum2.y = fmaf(f, y.y, sum2.y);
             }
             if (whole) {
-              *reinterpret_cast<uint32_t*>(out + token_head(row) + c) = Num<T>::from2(sum2.x / l, sum2.y / l);
+              *reinterpret_cast<uint32_t*>(out + row_offset(V, at, row) + c) = Num<T>::from2(sum2.x / l, sum2.y / l);
             } else {
               *reinterpret_cast<float2*>(part + (size_t)row * (D + 4) + c) = sum2;
               if (c == 0) *reinterpret_cast<float2*>(part + (size_t)row * (D + 4) + D) = make_float2(top, l);
@@ -598,7 +454,7 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
           const int r = wr * 16 + g + 8 * h;
           if (r >= rows) continue;
           if (whole) {
-            T* to = out + token_head(r) + 2 * t4;
+            T* to = out + row_offset(V, at, r) + 2 * t4;
             const float inv = 1.f / all[h];
 #pragma unroll
             for (int j = 0; j < kTiles; ++j)
@@ -726,20 +582,24 @@ kv_join_kernel(KvView V, T* out) {
   if (blockIdx.x == 0 && threadIdx.x == 0) V.counts[KV_TAKEN] = 0;
 }
 
-// What to do with the kernel for a type, head dimension and row tiles: few rows leave the tile's keys to more warps.
+// What to do with the kernels for a type, head dimension and row tiles: few rows leave the tile's keys to more warps.
+// Heads of 64 and 128 come here with up to 16 rows; more are the wide kernel's.
 template <typename T, int D, int WR, int WK, typename F>
 cudaError_t with(F f) {
   using S = Shape<D, WR, WK>;
-  return f(kv_attention_kernel<T, D, WR, WK>, kv_join_kernel<T, D>, S::kThreads, S::kSmem, (T*)nullptr);
+  return f(kv_attention_kernel<T, D, WR, WK>, S::kThreads, S::kSmem);
 }
 template <typename T, int D, typename F>
 cudaError_t with_rows(int row_tiles, F f) {
-  if (row_tiles == 1) return with<T, D, 1, 4>(f);
-  if constexpr (D <= 128) {
+  if constexpr (D == 64 || D == 128) {
+    return with<T, D, 1, 4>(f);
+  } else if constexpr (D < 128) {
+    if (row_tiles == 1) return with<T, D, 1, 4>(f);
     if (row_tiles == 2) return with<T, D, 2, 4>(f);
     if (row_tiles == 4) return with<T, D, 4, 2>(f);
     return with<T, D, 8, 1>(f);
   } else {                               // 128 registers of output: four warps that compute
+    if (row_tiles == 1) return with<T, D, 1, 4>(f);
     if (row_tiles == 2) return with<T, D, 2, 2>(f);
     return with<T, D, 4, 1>(f);
   }
@@ -759,6 +619,17 @@ cudaError_t with_kernel(const lif_kv* kv, F f) {
   const lif_kv_desc& d = kv->desc;
   return d.dtype == LIF_TYPE_F16 ? with_dim<__half>(d.head_dim, kv->row_tiles, f)
                                  : with_dim<__nv_bfloat16>(d.head_dim, kv->row_tiles, f);
+}
+template <typename T>
+cudaError_t launch_join(const lif_kv* kv, void* out, cudaStream_t st) {
+  auto go = [&](auto kernel) { return launch_k2(kernel, dim3(kv->n_sm), dim3(kJoinThreads), 0, st, 1, 1, kv->v, (T*)out); };
+  switch (kv->desc.head_dim) {
+    case 64: return go(kv_join_kernel<T, 64>);
+    case 80: return go(kv_join_kernel<T, 80>);
+    case 96: return go(kv_join_kernel<T, 96>);
+    case 128: return go(kv_join_kernel<T, 128>);
+    default: return go(kv_join_kernel<T, 256>);
+  }
 }
 
 // The pool as the tensor copies see it: a box is `columns` wide and as many rows as a tile takes of a page.
@@ -784,18 +655,20 @@ bool encode_map(CUtensorMap* map, const lif_kv_desc& d, int columns, CUtensorMap
 }  // namespace
 
 // Smallest block of rows that holds a key-value head's rows of one sequence, so that its keys are
-// read once, up to what registers and shared memory take (128 rows, 64 at 256 columns).
+// read once, up to what registers and shared memory take (128 rows, 64 at 256 columns).  The wide kernel's
+// blocks are the 128 rows of a tensor-core tile however few are there.
 int kv_row_tiles(const lif_kv_desc& d) {
   const int rows = d.n_heads / d.n_kv_heads * d.max_new, most = d.head_dim <= 128 ? 8 : 4;
   int t = 1;
   while (t < most && t * 16 < rows) t *= 2;
-  return t;
+  return t > 1 && (d.head_dim == 64 || d.head_dim == 128) ? most : t;
 }
 
 bool kv_attention_configure(lif_kv* kv, int* ctas_per_sm) {
   if (!encode_map(&kv->maps.wide, kv->desc, 64, CU_TENSOR_MAP_SWIZZLE_128B)) return false;
   if (kv->desc.head_dim == 96 && !encode_map(&kv->maps.rest, kv->desc, 32, CU_TENSOR_MAP_SWIZZLE_64B)) return false;
-  return with_kernel(kv, [&](auto kernel, auto, int threads, int smem, auto) {
+  if (kv_is_wide(kv->desc)) return kv_wide_configure(kv, ctas_per_sm) == cudaSuccess;
+  return with_kernel(kv, [&](auto kernel, int threads, int smem) {
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(ctas_per_sm, kernel, threads, smem);
     return e;
@@ -810,11 +683,11 @@ cudaError_t launch_kv_attention(const lif_kv* kv, int layer, const void* q, void
   a.scale_log2 = kv->scale * 1.4426950408889634f;
   a.layer = layer;
   a.pages = (const char*)d.dev_pages + (size_t)layer * d.n_pages * kv_page_elems(d) * 2;
-  return with_kernel(kv, [&](auto kernel, auto join, int threads, int smem, auto* type) {
-    cudaError_t e = launch_k2(kernel, dim3(kv->v.ctas), dim3(threads), smem, st, 1, 1, kv->maps, kv->v, a);
-    if (e == cudaSuccess) e = launch_k2(join, dim3(kv->n_sm), dim3(kJoinThreads), 0, st, 1, 1, kv->v, (decltype(type))out);
-    return e;
+  cudaError_t e = kv_is_wide(d) ? launch_kv_attention_wide(kv, a, st) : with_kernel(kv, [&](auto kernel, int threads, int smem) {
+    return launch_k2(kernel, dim3(kv->v.ctas), dim3(threads), smem, st, 1, 1, kv->maps, kv->v, a);
   });
+  if (e != cudaSuccess) return e;
+  return d.dtype == LIF_TYPE_F16 ? launch_join<__half>(kv, out, st) : launch_join<__nv_bfloat16>(kv, out, st);
 }
 
 }  // namespace lif

@@ -82,8 +82,9 @@ inline int kv_slot_rows(const lif_kv_desc& d) {
   const int rows = d.n_heads / d.n_kv_heads * d.max_new, block = 16 * kv_row_tiles(d);
   return rows < block ? rows : block;
 }
-// Runs of the attention kernel's work at most: where a block has few rows, further ones beside a CTA's first.
-inline int kv_max_runs(const lif_kv_desc& d) { return kv_row_tiles(d) <= 2 ? kKvMaxRuns : kKvMaxCtas; }
+// Runs of the attention kernel's work at most: where a block has few rows (and what its pieces leave
+// behind is small), further ones beside a CTA's first.
+inline int kv_max_runs(const lif_kv_desc& d) { return kv_slot_rows(d) <= 32 ? kKvMaxRuns : kKvMaxCtas; }
 // Tensor maps, and CTAs per SM of the attention kernel for this cache
 bool kv_attention_configure(lif_kv* kv, int* ctas_per_sm);
 cudaError_t launch_kv_append(const lif_kv* kv, int layer, const lif_kv_rows& q, const lif_kv_rows& k,
