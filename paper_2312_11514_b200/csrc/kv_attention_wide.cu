@@ -22,7 +22,9 @@
 // and where a value is not finite that some rows see and others do not, the tile's second product is formed
 // one by one outside the tensor cores (0 times infinity is not 0).
 //
-// Precision as in kv_attention.cu; sums run over a row's keys in their order.
+// Precision as in kv_attention.cu, but for the sum of a row's weights, which is that of the weights before
+// their rounding (the exponentials and these sums are the bound here): each weight's rounding, at most half a unit in
+// its last place, then stands in the output as it does in the weights.
 #include "kv_attention.cuh"
 
 namespace lif {
@@ -31,20 +33,28 @@ namespace {
 constexpr int kWideRows = 128, kHalfThreads = 192, kWideThreads = 2 * kHalfThreads, kInfos = 8;
 constexpr int kScoreColumns = kKvTile, kOutColumn = 2 * kKvTile, kColumns = 256;   // of tensor memory, a half
 
+constexpr int kMaxStages = 4;
 template <int D>
 struct Wide {
   static constexpr int kTileBytes = kKvTile * D * 2;                     // keys, or values
-  static constexpr int kQueryBytes = kWideRows * D * 2;
-  static constexpr int kFixed = kQueryBytes + 1024;
-  static constexpr int kRoom = (113 * 1024 - kFixed) / (2 * kTileBytes);
-  static constexpr int kStages = kRoom > 4 ? 4 : kRoom;                  // of keys, and of values
-  static constexpr int kHalfBytes = 2 * kStages * kTileBytes + kFixed, kSmem = 2 * kHalfBytes;
-  static_assert(kStages >= 2 && kInfos >= kStages + 3 && kOutColumn + D <= kColumns, "");
+  // The tile of queries has 128 rows for the tensor cores; memory is laid out for those that can be there, and
+  // rows behind them are whatever the ring holds there (a row's scores are its own).  What that saves are more stages.
+  static constexpr int kRoom = (227 * 1024 / 2 - 1024) / 1024 * 1024;    // of a half, beside its state
+  static int rows(int slot_rows) { return slot_rows <= 32 ? 32 : slot_rows <= 64 ? 64 : kWideRows; }
+  static int stages(int slot_rows) {
+    const int n = (kRoom - rows(slot_rows) * D * 2) / (2 * kTileBytes);
+    return n > kMaxStages ? kMaxStages : n;
+  }
+  static constexpr int kHalfBytes = kRoom + 1024, kSmem = 2 * kHalfBytes;
+  static_assert(kRoom - kWideRows * D * 2 >= 4 * kTileBytes && kInfos >= kMaxStages + 3 && kOutColumn + D <= kColumns, "");
+};
+struct WideShape {
+  int rows, stages;                // of queries; of keys, and of values
 };
 
 struct __align__(16) WideState {
   StageInfo info[kInfos];
-  uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4];
+  uint64_t k_full[kMaxStages], k_empty[kMaxStages], v_full[kMaxStages], v_empty[kMaxStages];
   uint64_t q_full, q_empty;        // rows of queries: here; read by the last product that needs them
   uint64_t s_full[2], p_full[2];   // scores; weights (and cleared values)
   uint64_t o_done, o_empty;        // a tile's second product; the output, read
@@ -115,11 +125,17 @@ __device__ __forceinline__ bool elect() {
 // (bounded; the warp's lanes go on, or give up, together)
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, unsigned parity) { return __all_sync(~0u, mbar_wait(bar, parity)); }
 
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  unsigned long long r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(*reinterpret_cast<unsigned long long*>(&a)), "l"(*reinterpret_cast<unsigned long long*>(&b)));
+  return *reinterpret_cast<float2*>(&r);
+}
+
 // ---- the loading warp -----------------------------------------------------------------------------------
 
 template <typename T, int D>
 __device__ __forceinline__ bool wide_feed(const KvMaps& maps, const KvView& V, const AttendArgs& a, uint32_t keys, uint32_t values,
-                                          unsigned char* queries, WideState* st, int who, int4 plan, int4 step) {
+                                          unsigned char* queries, WideState* st, WideShape shape, int who, int4 plan, int4 step) {
   using S = Wide<D>;
   constexpr int kChunks = D / 64;
   const int lane = threadIdx.x & 31;
@@ -139,7 +155,7 @@ __device__ __forceinline__ bool wide_feed(const KvMaps& maps, const KvView& V, c
     if (p < n_pages)
       tensor_g2s(values + v_stage * S::kTileBytes + chunk * 8192 + p * box * 128, &maps.wide, chunk * 64, row, V.n_kv_heads + head,
                  page, a.layer, st->v_full + v_stage);
-    if (++v_stage == S::kStages) v_stage = 0, v_turn ^= 1;
+    if (++v_stage == shape.stages) v_stage = 0, v_turn ^= 1;
     ++issued_v;
     return true;
   };
@@ -160,7 +176,7 @@ __device__ __forceinline__ bool wide_feed(const KvMaps& maps, const KvView& V, c
     if (p < next_n)
       tensor_g2s(keys + k_stage * S::kTileBytes + chunk * 8192 + p * box * 128, &maps.wide, chunk * 64, next_row, next_head, next_page,
                  a.layer, st->k_full + k_stage);
-    if (++k_stage == S::kStages) k_stage = 0, k_turn ^= 1;
+    if (++k_stage == shape.stages) k_stage = 0, k_turn ^= 1;
     // the values of the tile before
     if (i > 0 && !values_of()) {
       ++i;
@@ -178,16 +194,19 @@ __device__ __forceinline__ bool wide_feed(const KvMaps& maps, const KvView& V, c
         break;
       }
       const int row0 = at.block * kWideRows, rows = min(kWideRows, at.news * V.group - row0);
-      StageInfo info;
-      info.b = at.b;
-      info.head = at.head;
-      info.row0 = row0;
-      // lanes along a row's 16-byte pieces: [64 columns][row][128 bytes], permuted as the keys are
+      // lanes along a row's 16-byte pieces: [64 columns][row][128 bytes], permuted as the keys are; row r is head
+      // (row0 + r) % group of token (row0 + r) / group
       constexpr int kPieces = D / 8, kAtOnce = 32 / kPieces;
       const int c = lane % kPieces;
-      for (int r = lane / kPieces; r < rows; r += kAtOnce) {
-        const T* src = reinterpret_cast<const T*>(a.q) + row_offset(V, info, r) + 8 * c;
-        copy_async16(queries + (c / 8) * kWideRows * 128 + r * 128 + ((c & 7) ^ (r & 7)) * 16, src);
+      int r = lane / kPieces, t = (row0 + r) / V.group, h = row0 + r - t * V.group;
+      const T* src = reinterpret_cast<const T*>(a.q) + (((int64_t)at.b * V.max_new + t) * V.n_heads + at.head * V.group + h) * D + 8 * c;
+      const int64_t next_token = (int64_t)(V.n_heads - V.group) * D;
+      unsigned char* to = queries + (c / 8) * shape.rows * 128 + r * 128;
+#pragma unroll 4
+      for (; r < rows; r += kAtOnce, to += kAtOnce * 128) {
+        copy_async16(to + ((c & 7) ^ (r & 7)) * 16, src);
+        src += kAtOnce * D;
+        for (h += kAtOnce; h >= V.group; h -= V.group) src += next_token;
       }
       asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&st->q_full)) : "memory");
       ++piece;
@@ -196,14 +215,14 @@ __device__ __forceinline__ bool wide_feed(const KvMaps& maps, const KvView& V, c
   }
   if (ok) ok = values_of();
   // nobody leaves while copies are on their way
-  for (int k = 0; k < min(i, S::kStages); ++k) {
+  for (int k = 0; k < min(i, shape.stages); ++k) {
     if (k_stage == 0) k_turn ^= 1;
-    k_stage = k_stage == 0 ? S::kStages - 1 : k_stage - 1;
+    k_stage = k_stage == 0 ? shape.stages - 1 : k_stage - 1;
     mbar_wait(st->k_full + k_stage, k_turn);
   }
-  for (int k = 0; k < min(issued_v, S::kStages); ++k) {
+  for (int k = 0; k < min(issued_v, shape.stages); ++k) {
     if (v_stage == 0) v_turn ^= 1;
-    v_stage = v_stage == 0 ? S::kStages - 1 : v_stage - 1;
+    v_stage = v_stage == 0 ? shape.stages - 1 : v_stage - 1;
     mbar_wait(st->v_full + v_stage, v_turn);
   }
   own_copies_wait();
@@ -215,7 +234,7 @@ __device__ __forceinline__ bool wide_feed(const KvMaps& maps, const KvView& V, c
 // where the tensor cores' instructions take their operands from (MMA_FIGURE).
 
 template <typename T, int D>
-__device__ __forceinline__ bool wide_products(uint32_t keys, uint32_t values, uint32_t queries, WideState* st, uint32_t columns) {
+__device__ __forceinline__ bool wide_products(uint32_t keys, uint32_t values, uint32_t queries, WideState* st, WideShape shape, uint32_t columns) {
   using S = Wide<D>;
   const uint64_t q0 = operand(queries, 16), k0 = operand(keys, 16), v0 = operand(values, 8192);
   int k_stage = 0, v_stage = 0, piece_s = 0, piece_o = 0, flags_before = 0;
@@ -248,7 +267,7 @@ __device__ __forceinline__ bool wide_products(uint32_t keys, uint32_t values, ui
     }
     __syncwarp();
     add = true;
-    if (++v_stage == S::kStages) v_stage = 0, v_turn ^= 1;
+    if (++v_stage == shape.stages) v_stage = 0, v_turn ^= 1;
     return true;
   };
   for (int i = 0;; ++i) {
@@ -263,14 +282,14 @@ __device__ __forceinline__ bool wide_products(uint32_t keys, uint32_t values, ui
       const uint64_t k = k0 + k_stage * (S::kTileBytes >> 4);
 #pragma unroll
       for (int e = 0; e < D / 16; ++e)
-        mma_ss(columns + (i & 1) * kScoreColumns, q0 + ((e / 4) * kWideRows * 128 + (e % 4) * 32 >> 4),
+        mma_ss(columns + (i & 1) * kScoreColumns, q0 + (e / 4) * (shape.rows * 128 >> 4) + ((e % 4) * 32 >> 4),
                k + ((e / 4) * 8192 + (e % 4) * 32 >> 4), product<T>(kKvTile, false), e > 0);
       products_done(st->s_full + (i & 1));
       products_done(st->k_empty + k_stage);
       if (flags & kCloses) products_done(&st->q_empty);
     }
     __syncwarp();
-    if (++k_stage == S::kStages) k_stage = 0, k_turn ^= 1;
+    if (++k_stage == shape.stages) k_stage = 0, k_turn ^= 1;
     if (i > 0 && !second(i - 1, flags_before)) return false;
     flags_before = flags;
     if (flags & kLast) return second(i, flags);
@@ -281,7 +300,7 @@ __device__ __forceinline__ bool wide_products(uint32_t keys, uint32_t values, ui
 
 template <typename T, int D>
 __device__ __forceinline__ bool wide_rows(const KvView& V, const AttendArgs& a, unsigned char* values, WideState* st,
-                                          uint32_t columns, int warp) {
+                                          WideShape shape, uint32_t columns, int warp) {
   using S = Wide<D>;
   const int lane = threadIdx.x & 31, r = warp * 32 + lane;
   const uint32_t mine = columns + ((uint32_t)(warp * 32) << 16);
@@ -377,15 +396,16 @@ __device__ __forceinline__ bool wide_rows(const KvView& V, const AttendArgs& a, 
       }
       const float base = m == -INFINITY ? 0.f : m;
       uint32_t w[32];
-      float add4[4] = {0.f, 0.f, 0.f, 0.f};
+      float2 add[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+      const float2 factor = make_float2(a.scale_log2, a.scale_log2), offset = make_float2(-base, -base);
 #pragma unroll
       for (int c = 0; c < 32; ++c) {
-        w[c] = Num<T>::from2(power(fmaf(s[2 * c], a.scale_log2, -base)), power(fmaf(s[2 * c + 1], a.scale_log2, -base)));
-        const float2 used = Num<T>::to2(w[c]);
-        add4[(2 * c) & 3] += used.x;
-        add4[(2 * c + 1) & 3] += used.y;
+        const float2 e = fma2(make_float2(s[2 * c], s[2 * c + 1]), factor, offset);
+        const float2 p = make_float2(power(e.x), power(e.y));
+        w[c] = Num<T>::from2(p.x, p.y);
+        add[c & 1] = add2(add[c & 1], p);
       }
-      sum += (add4[0] + add4[1]) + (add4[2] + add4[3]);
+      sum += (add[0].x + add[0].y) + (add[1].x + add[1].y);
       if (!one_by_one) {
         columns_store(scores, w);
       } else {
@@ -432,7 +452,7 @@ __device__ __forceinline__ bool wide_rows(const KvView& V, const AttendArgs& a, 
     tensor_before();
     __syncwarp();
     if (lane == 0) mbar_arrive(st->p_full + half);
-    if (++v_stage == S::kStages) v_stage = 0, v_turn ^= 1;
+    if (++v_stage == shape.stages) v_stage = 0, v_turn ^= 1;
 
     if (at.flags & kCloses) {
       if (!done_through(i)) return false;
@@ -474,20 +494,20 @@ __device__ __forceinline__ bool wide_rows(const KvView& V, const AttendArgs& a, 
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kWideThreads, 1)
-kv_attention_wide_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a) {
+kv_attention_wide_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a, WideShape shape) {
   using S = Wide<D>;
   extern __shared__ __align__(1024) unsigned char smem[];
   // A warp reaches the tensor memory lanes of its number modulo 4, so rows are warps 0-3 of one half and 8-11 of
   // the other; 4-7 load and issue.
   const int number = __shfl_sync(~0u, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int half = number >= 6, role = number < 4 ? 0 : number >= 8 ? 0 : number % 2 == 0 ? 4 : 5;
-  unsigned char *keys = smem + half * S::kHalfBytes, *values = keys + S::kStages * S::kTileBytes,
-                *queries = values + S::kStages * S::kTileBytes;
-  WideState* st = reinterpret_cast<WideState*>(queries + S::kQueryBytes);
+  unsigned char *queries = smem + half * S::kHalfBytes, *keys = queries + shape.rows * D * 2,
+                *values = keys + shape.stages * S::kTileBytes;
+  WideState* st = reinterpret_cast<WideState*>(queries + S::kRoom);
   WideState* first = reinterpret_cast<WideState*>(reinterpret_cast<unsigned char*>(st) - half * S::kHalfBytes);
   if (role == 4 && lane == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.wide) : "memory");
-    for (int i = 0; i < S::kStages; ++i) {
+    for (int i = 0; i < shape.stages; ++i) {
       mbar_init(st->k_full + i, 1);
       mbar_init(st->k_empty + i, 1);
       mbar_init(st->v_full + i, 1);
@@ -523,13 +543,13 @@ kv_attention_wide_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendAr
   if (who < step.y) {
     bool ok = true;
     if (role == 4) {
-      ok = wide_feed<T, D>(maps, V, a, smem_u32(keys), smem_u32(values), queries, st, who, plan, step);
+      ok = wide_feed<T, D>(maps, V, a, smem_u32(keys), smem_u32(values), queries, st, shape, who, plan, step);
     } else if (role == 5) {
-      ok = wide_products<T, D>(smem_u32(keys), smem_u32(values), smem_u32(queries), st, columns);
+      ok = wide_products<T, D>(smem_u32(keys), smem_u32(values), smem_u32(queries), st, shape, columns);
       if (elect()) products_done(&st->drained);      // none is under way when the columns are given back
       warp_wait(&st->drained, 0);
     } else {
-      ok = wide_rows<T, D>(V, a, values, st, columns, number % 4);
+      ok = wide_rows<T, D>(V, a, values, st, shape, columns, number % 4);
     }
     if (!ok) flag_timeout(V.counts + LIF_KV_CNT_STATUS);
   }
@@ -540,19 +560,22 @@ kv_attention_wide_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendAr
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(all), "n"(2 * kColumns) : "memory");
 }
 
+template <int D, typename T, typename F>
+cudaError_t with(const lif_kv* kv, F f) {
+  using S = Wide<D>;
+  return f(kv_attention_wide_kernel<T, D>, S::kSmem, WideShape{S::rows(kv->v.slot_rows), S::stages(kv->v.slot_rows)});
+}
 template <typename F>
-auto with_wide(const lif_kv* kv, F f) {
+cudaError_t with_wide(const lif_kv* kv, F f) {
   const bool half = kv->desc.dtype == LIF_TYPE_F16;
-  if (kv->desc.head_dim == 64)
-    return half ? f(kv_attention_wide_kernel<__half, 64>, Wide<64>::kSmem) : f(kv_attention_wide_kernel<__nv_bfloat16, 64>, Wide<64>::kSmem);
-  return half ? f(kv_attention_wide_kernel<__half, 128>, Wide<128>::kSmem)
-              : f(kv_attention_wide_kernel<__nv_bfloat16, 128>, Wide<128>::kSmem);
+  if (kv->desc.head_dim == 64) return half ? with<64, __half>(kv, f) : with<64, __nv_bfloat16>(kv, f);
+  return half ? with<128, __half>(kv, f) : with<128, __nv_bfloat16>(kv, f);
 }
 
 }  // namespace
 
 cudaError_t kv_wide_configure(const lif_kv* kv, int* ctas_per_sm) {
-  return with_wide(kv, [&](auto kernel, int smem) {
+  return with_wide(kv, [&](auto kernel, int smem, WideShape) {
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(ctas_per_sm, kernel, kWideThreads, smem);
     if (e == cudaSuccess && *ctas_per_sm > 0) *ctas_per_sm = 2;          // two halves
@@ -561,8 +584,8 @@ cudaError_t kv_wide_configure(const lif_kv* kv, int* ctas_per_sm) {
 }
 
 cudaError_t launch_kv_attention_wide(const lif_kv* kv, const AttendArgs& a, cudaStream_t st) {
-  return with_wide(kv, [&](auto kernel, int smem) {
-    return launch_k2(kernel, dim3(kv->v.ctas / 2), dim3(kWideThreads), smem, st, 1, 1, kv->maps, kv->v, a);
+  return with_wide(kv, [&](auto kernel, int smem, WideShape shape) {
+    return launch_k2(kernel, dim3(kv->v.ctas / 2), dim3(kWideThreads), smem, st, 1, 1, kv->maps, kv->v, a, shape);
   });
 }
 
