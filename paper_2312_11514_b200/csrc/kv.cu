@@ -10,7 +10,8 @@
 //                       round trips (lengths; last pages and the first free ones; references)
 //   kv_arrange_kernel   fork and load: tables of up to kSmallPages pages and kSmallTable entries in one
 //                       CTA, references counted in shared memory; larger ones in a cluster of eight, whose
-//                       barrier separates the phases in place of launches.  COMPARE_FIGURES
+//                       barrier separates the phases in place of launches (64 places of ten pages,
+//                       loaded and compacted: 28 us in clusters, 15 us so)
 //   kv_compact_kernel   likewise (kv_compact_small_kernel: one CTA, lists and new ids in shared memory)
 //   kv_copy_pages_kernel  what reserve and compact decided to copy, all layers; a warp per 4 KB
 //
@@ -577,7 +578,9 @@ __global__ void kv_clear_kernel(KvView v) {
 }
 
 // Rows of pages list_a[i] to pages list_b[i], every layer and head.  Unit: 4 KB of one head's rows, a
-// warp, eight 16-byte loads of a lane on their way together.
+// warp, eight 16-byte loads of a lane on their way together, the stores marked as not read again (82 MB of 16-row
+// beams' pages: 33 us with the calls ahead of it, 37 without the mark; 0.55 GB: 182 us, 92% of measured HBM, with
+// sixteen CTAs an SM to follow one another where four that stayed took 193).
 constexpr int kCopyUnit = 4096;
 __global__ void __launch_bounds__(kThreads)
 kv_copy_pages_kernel(KvView v, uint4* pages, int n_layers, int head_bytes, int units_per_head) {
@@ -603,7 +606,7 @@ kv_copy_pages_kernel(KvView v, uint4* pages, int n_layers, int head_bytes, int u
       if ((k * 32 + lane) * 16 < bytes) x[k] = ld_stream16(s + k * 32 + lane);
 #pragma unroll
     for (int k = 0; k < kCopyUnit / 512; ++k)
-      if ((k * 32 + lane) * 16 < bytes) d[k * 32 + lane] = x[k];
+      if ((k * 32 + lane) * 16 < bytes) __stcs(d + k * 32 + lane, x[k]);
   }
 }
 
@@ -620,7 +623,7 @@ cudaError_t launch_arrange(const lif_kv* kv, const int32_t* from, const int32_t*
 cudaError_t launch_copies(const lif_kv* kv, cudaStream_t st) {
   const lif_kv_desc& d = kv->desc;
   const int head_bytes = d.page_tokens * d.head_dim * 2;
-  return launch_k(kv_copy_pages_kernel, dim3(kv->n_sm * 4), dim3(kThreads), 0, st, 1, kv->v, (uint4*)d.dev_pages,
+  return launch_k(kv_copy_pages_kernel, dim3(kv->n_sm * 16), dim3(kThreads), 0, st, 1, kv->v, (uint4*)d.dev_pages,
                   d.n_layers, head_bytes, (head_bytes + kCopyUnit - 1) / kCopyUnit);
 }
 

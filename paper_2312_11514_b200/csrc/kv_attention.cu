@@ -3,13 +3,16 @@
 //   out[row] = sum_j w_j v_j / sum_j w_j,   w_j = exp(scale <q_row, k_j> - max_j)
 //
 // Rows: the new tokens' query heads that share a key-value head, `group` x tokens of them (1 .. 16
-// mostly), in blocks of 16 x WR.  Every key and value is read once per row block; bound: HBM, until
-// rows x heads make the tensor cores or the exponentials one (a single key-value head under many query heads).
+// mostly), in blocks of 16 x WR (more than 16 rows of 64 or 128 elements: kv_attention_wide.cu).  Every key and
+// value is read once per row block; bound: HBM (64 sequences of 300 .. 4000 under 56 heads of 128: 2.5 GB in 359 us,
+// 1.05 of measured; 8 ragged ones: 59 us, 94%), and latency where the step is small: one sequence of 1000 under 32
+// heads takes 7.6 us, 2.5 of them its bytes (table and plan 1, first copy 1, two tiles 1.6, their sum 0.6, join 2.4).
 //
 // Split.  The step's work is numbered in tiles of 64 keys (kv_plan) and cut into runs, across heads and
 // sequences, so that one long sequence, many short ones and anything ragged between fill the chip alike.
 // Every CTA begins with a run of its own; where the work is long these cover three quarters of it and the
-// rest is taken in short runs by whoever is free (SCHEDULE_FIGURES).  A head that a run's end cuts is
+// rest is taken in short runs by whoever is free: CTAs with equal work differ by a fifth in time (memory is nearer to
+// some pages than to others), and 64 sequences of 56 heads went from 451 to 360 us.  A head that a run's end cuts is
 // finished by kv_join_kernel from the pieces' {max, sum, unnormalised output}.  Which run holds which tiles
 // does not depend on who takes it, and pieces are joined in their order: the same bits every time.
 //
@@ -475,7 +478,8 @@ constexpr int kJoinThreads = 512;
 // Finishes the heads that the runs' ends cut: some warps of a CTA per head and row, as many as there are warps
 // for, lanes along the columns, pieces dealt to the warps and joined in a fixed order.  The lists are those
 // of the step, written before the kernel ahead passed its own wait; the pieces are that kernel's.  Bound:
-// latency (a round trip for eight pieces a warp).
+// latency (a round trip for eight pieces a warp): 1.5 us for 32 heads of 8 pieces, 5 us for 32 rows of 220.  A ticket
+// per head in the kernel ahead, whose last piece's CTA did this, took 1.2 us a piece and 20 us for 71 rows of 18.
 template <typename T, int D>
 __global__ void __launch_bounds__(kJoinThreads)
 kv_join_kernel(KvView V, T* out) {

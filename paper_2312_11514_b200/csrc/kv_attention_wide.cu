@@ -1,10 +1,13 @@
 // Attention over the paged cache where more than 16 rows share a key-value head (a long step, many query heads
 // over few), head dimensions 64 and 128: the formula, the split into runs and the join are kv_attention.cu's.
 //
-// Why another kernel.  One row block of 128 is a tile of the tcgen05 tensor cores: a tile of 64 keys costs them
-// 2 x D / 64 x 64 clocks, where mma.sync takes eight times as long and was the bound.  What is left is one
-// exponential per row and key (16 a clock and SM): with 128 rows a tile of 64 keys takes 512 clocks of those, as
-// long as its 16 D bytes a key take HBM for D = 128.  Few rows leave lanes of the softmax idle but cost no more time.
+// Why another kernel.  One row block of 128 is a tile of the tcgen05 tensor cores, where mma.sync took eight
+// times as long and was the bound: 64 new tokens of 4 sequences of 8000, 32 heads over 8, 125 us there and 69 here
+// (two row blocks read keys and values each: 262 MB, 58% of measured HBM); 4 tokens of
+// 64 heads over 8, 16 sequences of 4000, 85 and 66; 71 heads over one of 64, 8 sequences of 60000, 65 and 39.  Only the
+// shortest lose: 71 heads, 8 sequences of 1500 .. 32000, 16.1 and 17.0 (lengths are known on the device alone).  What
+// is left is one exponential per row and key (16 a clock and SM): with 128 rows a tile of 64 keys takes 512 clocks of
+// those, two thirds of what its bytes take HBM for D = 128.  Few rows leave lanes of the softmax idle but cost no more.
 // A CTA is two halves of six warps that share nothing but the allocation of tensor memory, so that one's tensor
 // cores and copies run beside the other's exponentials.  (Two CTAs an SM would do the same, but the allocation waits
 // without a limit where CTAs compete for it; one CTA takes all 512 columns at once.)  In a half:
@@ -231,7 +234,7 @@ __device__ __forceinline__ bool wide_feed(const KvMaps& maps, const KvView& V, c
 
 // ---- the warp that issues the products ------------------------------------------------------------------------
 // All its lanes walk and wait, one issues: what it computes is the warp's and stays in uniform registers, which is
-// where the tensor cores' instructions take their operands from (MMA_FIGURE).
+// where the tensor cores' instructions take their operands from (one lane alone: 2000 clocks a tile, so: 900).
 
 template <typename T, int D>
 __device__ __forceinline__ bool wide_products(uint32_t keys, uint32_t values, uint32_t queries, WideState* st, WideShape shape, uint32_t columns) {

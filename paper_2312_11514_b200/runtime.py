@@ -255,6 +255,8 @@ class KvCache:
             self._expect("q_out", q_out, self._queries)
         weights = None
         if self.norm != B.NORM_NONE and norms is not None:
+            if len(norms) != 4:
+                raise ValueError(f"KvCache: {len(norms)} norm tensors; expected query weight and bias, key weight and bias")
             for t in norms:
                 if t is not None:
                     self._expect("norm weight", t, self._head)
