@@ -157,8 +157,10 @@ lif_status lif_kv_append(lif_kv* kv, int32_t layer, const lif_kv_rows* q, const 
  *   out[b][t][i] = sum_j w_j v_j / sum_j w_j,  w_j = exp(scale <q[b][t][i], k_j> - max_j ...),
  * j over the tokens that the position of token t sees.  dev_q and dev_out: [max_seqs][max_new]
  * [n_heads][head_dim], 16-byte aligned; rows t >= n_new[b] are neither read nor written.  dev_out may
- * not overlap dev_q.  What a token does not see never enters its result, infinities and NaN included.
- * The same cache, tables and inputs give the same bits. */
+ * not overlap dev_q.  What a token does not see never enters its result, infinities and NaN included
+ * (rows of a sequence's pages that no token sees may be read all the same).
+ * The same cache, tables and inputs give the same bits.  Waits inside the kernels are bounded: one that ran
+ * out sets LIF_ERR_TIMEOUT, over any other status, and that call's output is not to be used. */
 lif_status lif_kv_attention(lif_kv* kv, int32_t layer, const void* dev_q, void* dev_out, void* stream);
 
 /* Rearranges the places, all at once: afterwards place b holds the first dev_len[b] tokens of what
