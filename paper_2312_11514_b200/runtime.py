@@ -180,7 +180,7 @@ class KvCache:
         self._index = self.device.index if self.device.index is not None else torch.cuda.current_device()
         self._queries, self._keys = (max_seqs, max_new, n_heads, head_dim), (max_seqs, max_new, n_kv_heads, head_dim)
         self._places, self._table, self._head = (max_seqs,), (max_seqs, self.max_pages), (head_dim,)
-        self._lib = B.lib()
+        self._lib, self._both = B.lib(), max_seqs > 1 and max_new > 1
         shape = dict(n_layers=n_layers, n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim,
                      dtype=self._TYPES[dtype], page_tokens=page_tokens, n_pages=n_pages, max_seqs=max_seqs,
                      max_pages=self.max_pages, max_new=max_new, window=window, scale=scale or 0.0, norm=norm,
@@ -233,13 +233,14 @@ class KvCache:
         if t.get_device() != self._index or t.dtype is not self.dtype or t.shape != shape:
             self._expect(name, t, shape, contiguous=False)
         places, tokens, step, element = t.stride()
-        many, several = self.max_seqs > 1, self.max_new > 1
         # places lie max_new tokens apart
-        if element != 1 or (many and several and places != self.max_new * tokens):
+        if element != 1 or (self._both and places != self.max_new * tokens):
             raise ValueError(f"KvCache: {name} has strides {t.stride()}; places have to lie max_new tokens apart, "
                              f"a head's elements beside each other")
         # a KvRows (torch leaves the stride of a dimension of one element undefined)
-        return _ROWS(t.data_ptr(), tokens if several else places if many else 0, step if shape[2] > 1 else 0)
+        if self.max_new == 1:
+            tokens = places if self.max_seqs > 1 else 0
+        return _ROWS(t.data_ptr(), tokens, step if shape[2] > 1 else 0)
 
     def reserve(self, n_new: torch.Tensor, stream=None) -> None:
         B.lif_kv_reserve(self.handle, self._ints("n_new", n_new), self._on(stream))
@@ -249,20 +250,27 @@ class KvCache:
         """q ``[max_seqs][max_new][n_heads][head_dim]``, k and v with n_kv_heads; views into a fused
         projection's output are fine.  ``norms``: query weight, query bias, key weight, key bias.
         Returns the normed and rotated queries (rows of tokens that are not there are not written)."""
+        index, dtype, head = self._index, self.dtype, self._head
         if q_out is None:
-            q_out = torch.empty(self._queries, dtype=self.dtype, device=self.device)
+            q_out = torch.empty(self._queries, dtype=dtype, device=self.device)
         else:
             self._expect("q_out", q_out, self._queries)
         weights = None
-        if self.norm != B.NORM_NONE and norms is not None:
+        if self.norm and norms is not None:
             if len(norms) != 4:
                 raise ValueError(f"KvCache: {len(norms)} norm tensors; expected query weight and bias, key weight and bias")
+            at = []
             for t in norms:
-                if t is not None:
-                    self._expect("norm weight", t, self._head)
-            weights = _NORMS(*[0 if t is None else t.data_ptr() for t in norms])
+                if t is None:
+                    at.append(0)
+                    continue
+                if t.dtype is not dtype or t.get_device() != index or t.shape != head or not t.is_contiguous():
+                    self._expect("norm weight", t, head)
+                at.append(t.data_ptr())
+            weights = _NORMS(*at)
+        stream = torch._C._cuda_getCurrentRawStream(index) if stream is None else B._stream(stream)
         code = self._lib.lif_kv_append(self.handle, layer, self._rows("q", q, self._queries), self._rows("k", k, self._keys),
-                                       self._rows("v", v, self._keys), weights, q_out.data_ptr(), B._stream(self._on(stream)))
+                                       self._rows("v", v, self._keys), weights, q_out.data_ptr(), stream)
         if code:
             raise B.LifError(code, "lif_kv_append")
         return q_out
@@ -273,7 +281,8 @@ class KvCache:
             out = torch.empty_like(q)
         else:
             self._expect("out", out, self._queries)
-        code = self._lib.lif_kv_attention(self.handle, layer, q.data_ptr(), out.data_ptr(), B._stream(self._on(stream)))
+        stream = torch._C._cuda_getCurrentRawStream(self._index) if stream is None else B._stream(stream)
+        code = self._lib.lif_kv_attention(self.handle, layer, q.data_ptr(), out.data_ptr(), stream)
         if code:
             raise B.LifError(code, "lif_kv_attention")
         return out
