@@ -204,7 +204,7 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
   auto sync = [&]() {                                // the warps that compute; bounded as every wait
     __syncwarp();
     if (lane == 0) mbar_arrive(&bars->all);
-    return mbar_wait(&bars->all, syncs++ & 1, 2 * kWaitLimit);   // (a warp that still waits for a tile comes, or never will)
+    return (bool)__all_sync(~0u, mbar_wait(&bars->all, syncs++ & 1, 2 * kWaitLimit));   // (a warp that still waits for a tile comes, or never will)
   };
   auto release = [&](uint64_t* bar) {
     __syncwarp();
@@ -222,7 +222,7 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
   const int val_row = wk * kKeys + (lane & 15), val_b = lane >> 4;
 #pragma unroll 1
   for (bool last = false; !last;) {
-    if (!mbar_wait(bars->full + stage, turn)) {
+    if (!__all_sync(~0u, mbar_wait(bars->full + stage, turn))) {   // (the warp's lanes go on, or give up, together)
       if (lane == 0) flag_timeout(V.counts + LIF_KV_CNT_STATUS);
       return;
     }
