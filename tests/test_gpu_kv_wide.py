@@ -218,3 +218,58 @@ def test_norm_tensors_are_counted():
     with pytest.raises(ValueError, match="norm tensors"):
         kv.append(0, q, q, q, norms=[w, w])
     kv.close()
+
+
+def test_two_caches_with_wide_blocks_on_two_streams():
+    """Their kernels take the tensor memory of the SMs in turn; a third stream's narrow cache runs beside them."""
+    lens, news = [900, 90, 5000], [2, 1, 2]
+    made = [make(lens, news, seed=s, dim=128, heads=h, kv_heads=2) for s, h in ((1, 32), (2, 64), (3, 4))]
+    streams = [torch.cuda.Stream() for _ in made]
+    qs = [queries(kv, g) for kv, _, g in made]
+    outs = [torch.full_like(q, 7) for q in qs]
+    torch.cuda.synchronize()
+    for _ in range(30):
+        for (kv, _, _), q, out, s in zip(made, qs, outs, streams):
+            with torch.cuda.stream(s):
+                kv.attention(0, q, out=out)
+    for (kv, rows, _), q, out in zip(made, qs, outs):
+        torch.cuda.synchronize()
+        check_attention(kv, rows, lens, news, q, out)
+        assert kv.stats()["status"] == B.LIF_OK
+        kv.close()
+
+
+def test_the_last_page_of_the_pool_and_of_a_sequence():
+    """A reserve that takes every page, sequences that end at max_pages exactly, one token more refused; then attention
+    over all of it, a fork that changes nothing but ends the step, and freeing."""
+    page, max_pages, dim = 8, 4, 64
+    kv = R.KvCache(n_layers=1, n_heads=4, n_kv_heads=2, head_dim=dim, n_pages=8, max_seqs=2, max_pages=max_pages,
+                   page_tokens=page, max_new=32)
+    ref = K.Tables(2, max_pages, 8, page, 32)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(4)
+    kv.reserve(ints([32, 32]))
+    assert ref.reserve([32, 32])[0] is None
+    ref.check(kv)
+    assert kv.stats()["free"] == 0
+    q, k, v = queries(kv, g), queries(kv, g, 2), queries(kv, g, 2)
+    kv.append(0, q, k, v, q_out=q)
+    out = attend(kv, q)
+    check_attention(kv, ref.rows, [32, 32], [32, 32], q, out)
+    kv.fork()
+    ref.fork()
+    ref.check(kv)
+    assert (attend(kv, q) == 7).all()                       # no step under way
+    kv.reserve(ints([1, 0]))
+    assert ref.reserve([1, 0])[0] == "capacity" and kv.stats()["status"] == B.LIF_ERR_CAPACITY
+    ref.check(kv)
+    kv.clear_status()
+    kv.fork(ints([-1, 1]), ints([7, 25]))
+    ref.fork([-1, 1], [7, 25])
+    ref.check(kv)
+    kv.reserve(ints([5, 7]))
+    assert ref.reserve([5, 7])[0] is None
+    ref.check(kv)
+    out = attend(kv, q)
+    check_attention(kv, ref.rows, [5, 32], [5, 7], q, out)
+    kv.close()
