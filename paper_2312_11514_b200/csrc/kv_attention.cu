@@ -10,7 +10,7 @@
 //
 // Split.  The step's work is numbered in tiles of 64 keys (kv_plan) and cut into runs, across heads and
 // sequences, so that one long sequence, many short ones and anything ragged between fill the chip alike.
-// Every CTA begins with a run of its own; where the work is long these cover three quarters of it and the
+// Every CTA begins with a run of its own; where the work is long these cover most of it and the
 // rest is taken in short runs by whoever is free: CTAs with equal work differ by a fifth in time (memory is nearer to
 // some pages than to others), and 64 sequences of 56 heads went from 451 to 360 us.  A head that a run's end cuts is
 // finished by kv_join_kernel from the pieces' {max, sum, unnormalised output}.  Which run holds which tiles
