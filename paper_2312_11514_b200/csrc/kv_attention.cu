@@ -28,9 +28,10 @@
 // and the weights stay in registers from the first product to the second.  The WK warps of a row
 // are summed when the head ends.
 //
-// Precision.  Scores, maxima, sums and outputs are fp32.  Weights are rounded to the cache's type
-// for the second product (at most half a unit in the last place of each, like the rounding of the
-// output); the sum is that of the rounded weights, so that they add up to one exactly as they are used.
+// Precision.  Scores, references, sums and outputs are fp32.  Weights are rounded to the cache's type
+// for the second product: at most half a unit in the last place of each, like the rounding of the
+// output; in fp16, of a weight below 2^-21 of the row's largest, 2^-32 of that one.  The sum is that of
+// the rounded weights, so that they add up to one exactly as they are used.
 #include "kv_attention.cuh"
 
 namespace lif {
@@ -309,7 +310,7 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
 #pragma unroll
         for (int n = 1; n < kNT; ++n) top[h] = fmaxf(top[h], fmaxf(s[n][2 * h], s[n][2 * h + 1]));
         top[h] *= a.scale_log2;
-        above = above || top[h] > m[h] + kSlack;
+        above = above || too_far<T>(top[h], m[h]);
       }
       if (__any_sync(~0u, above)) {
         float shrink[2];
@@ -318,9 +319,9 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
           top[h] = fmaxf(top[h], __shfl_xor_sync(~0u, top[h], 1));
           top[h] = fmaxf(top[h], __shfl_xor_sync(~0u, top[h], 2));
           // (each row by itself: what a row gets must not depend on the others, which may not be there)
-          if (!(top[h] > m[h] + kSlack)) top[h] = m[h];
-          shrink[h] = power(m[h] - (top[h] == -INFINITY ? 0.f : top[h]));
-          m[h] = top[h];
+          const float now = too_far<T>(top[h], m[h]) ? top[h] - Num<T>::kLift : m[h];
+          shrink[h] = power(m[h] - (now == -INFINITY ? 0.f : now));
+          m[h] = now;
           sum[h] *= shrink[h];
         }
 #pragma unroll

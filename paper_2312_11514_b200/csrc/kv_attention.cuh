@@ -28,10 +28,16 @@ __device__ __forceinline__ float power(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// Weights refer to a score that need not be the row's maximum, only near enough that no weight is large (up to
-// 2^kSlack); it is brought up to date, and what was summed scaled down, when a score lies further above it.  The key
-// that set it has weight 1, so nothing gets smaller than with the maximum.
+// Weights are 2^(score - reference).  The reference need not be the row's maximum, only near enough that no weight is
+// too large; it is brought up to date, and what was summed scaled down, when a score lies more than kSlack above the
+// one that set it.  That one has weight 2^kLift, so nothing gets smaller than with the maximum.  The lift is for fp16,
+// which holds 2^-24 .. 65504: weights go up to 2^(kLift + kSlack) = 2^15, and what is far below the largest one
+// counts down to 2^-32 of it, where without the lift all keys below 2^-25 would be lost: a quarter (narrow kernel) to
+// nearly all (wide) of the output where one key of no value holds the weight and 131001 others lie there.  It costs nothing:
+// it stands in the reference.
 constexpr float kSlack = 8.f;
+template <typename T>
+__device__ __forceinline__ bool too_far(float score, float reference) { return score > reference + (kSlack + Num<T>::kLift); }
 
 // a box of the pool at {column, row in the page, operand and head, page, layer}
 __device__ __forceinline__ void tensor_g2s(uint32_t to, const CUtensorMap* map, int x, int row, int head, int page,

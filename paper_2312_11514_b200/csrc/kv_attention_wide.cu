@@ -26,8 +26,8 @@
 // one by one outside the tensor cores (0 times infinity is not 0).
 //
 // Precision as in kv_attention.cu, but for the sum of a row's weights, which is that of the weights before
-// their rounding (the exponentials and these sums are the bound here): each weight's rounding, at most half a unit in
-// its last place, then stands in the output as it does in the weights.
+// their rounding (the exponentials and these sums are the bound here): each weight's rounding then stands in the
+// output as it does in the weights.
 #include "kv_attention.cuh"
 
 namespace lif {
@@ -376,9 +376,9 @@ __device__ __forceinline__ bool wide_rows(const KvView& V, const AttendArgs& a, 
 #pragma unroll
       for (int c = 4; c < 64; ++c) top4[c & 3] = fmaxf(top4[c & 3], s[c]);
       const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3])) * a.scale_log2;
-      const bool above = top > m + kSlack;
+      const bool above = too_far<T>(top, m);
       if (__any_sync(~0u, above)) {                  // (each row by itself: rows that are not there hold anything)
-        const float now = above ? top : m;
+        const float now = above ? top - Num<T>::kLift : m;
         const float shrink = power(m - (now == -INFINITY ? 0.f : now));
         m = now;
         sum *= shrink;

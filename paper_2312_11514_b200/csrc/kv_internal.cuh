@@ -117,6 +117,7 @@ template <> struct Num<__half> {
   }
   static __device__ __forceinline__ float to1(unsigned short v) { return __half2float(__ushort_as_half(v)); }
   static constexpr uint32_t kExponent = 0x7c007c00u;   // all ones: infinite or NaN
+  static constexpr float kLift = 7.f;                  // of a softmax's weights (kv_attention.cuh)
 };
 template <> struct Num<__nv_bfloat16> {
   static __device__ __forceinline__ float2 to2(uint32_t v) { return __bfloat1622float2(*reinterpret_cast<__nv_bfloat162*>(&v)); }
@@ -126,6 +127,7 @@ template <> struct Num<__nv_bfloat16> {
   }
   static __device__ __forceinline__ float to1(unsigned short v) { return __bfloat162float(__ushort_as_bfloat16(v)); }
   static constexpr uint32_t kExponent = 0x7f807f80u;
+  static constexpr float kLift = 0.f;
 };
 #endif
 
