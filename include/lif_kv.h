@@ -160,7 +160,8 @@ lif_status lif_kv_append(lif_kv* kv, int32_t layer, const lif_kv_rows* q, const 
  * not overlap dev_q.  What a token does not see never enters its result, infinities and NaN included
  * (rows of a sequence's pages that no token sees may be read all the same).
  * The w_j are rounded to the cache's type: by half a unit in the last place, and with LIF_TYPE_F16 by up to 2^-32 of
- * the row's largest where they are below 2^-21 of it.
+ * the row's largest where they are below 2^-21 of it.  Scores scale <q, k> may be up to 10^8 in magnitude (beyond,
+ * fp32 is too coarse for a softmax in any case).
  * The same cache, tables and inputs give the same bits.  Waits inside the kernels are bounded: one that ran
  * out sets LIF_ERR_TIMEOUT, over any other status, and that call's output is not to be used. */
 lif_status lif_kv_attention(lif_kv* kv, int32_t layer, const void* dev_q, void* dev_out, void* stream);

@@ -309,8 +309,7 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
         top[h] = fmaxf(s[0][2 * h], s[0][2 * h + 1]);
 #pragma unroll
         for (int n = 1; n < kNT; ++n) top[h] = fmaxf(top[h], fmaxf(s[n][2 * h], s[n][2 * h + 1]));
-        top[h] *= a.scale_log2;
-        above = above || too_far<T>(top[h], m[h]);
+        above = above || too_far<T>(top[h], a.scale_log2, m[h]);
       }
       if (__any_sync(~0u, above)) {
         float shrink[2];
@@ -319,7 +318,7 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
           top[h] = fmaxf(top[h], __shfl_xor_sync(~0u, top[h], 1));
           top[h] = fmaxf(top[h], __shfl_xor_sync(~0u, top[h], 2));
           // (each row by itself: what a row gets must not depend on the others, which may not be there)
-          const float now = too_far<T>(top[h], m[h]) ? top[h] - Num<T>::kLift : m[h];
+          const float now = too_far<T>(top[h], a.scale_log2, m[h]) ? new_reference<T>(top[h], a.scale_log2) : m[h];
           shrink[h] = power(m[h] - (now == -INFINITY ? 0.f : now));
           m[h] = now;
           sum[h] *= shrink[h];

@@ -35,9 +35,16 @@ __device__ __forceinline__ float power(float x) {
 // counts down to 2^-32 of it, where without the lift all keys below 2^-25 would be lost: a quarter (narrow kernel) to
 // nearly all (wide) of the output where one key of no value holds the weight and 131001 others lie there.  It costs nothing:
 // it stands in the reference.
+// What is compared is the exponent of the row's largest weight, formed as every weight's is (one rounding; no weight
+// has a larger one), and a new reference is rounded up: then no exponent passes kLift + kSlack however coarse fp32 is
+// at that score.  (A product rounded on its own and a rounded reference + slack let weights of 2^16 through at 2^27.)
 constexpr float kSlack = 8.f;
 template <typename T>
-__device__ __forceinline__ bool too_far(float score, float reference) { return score > reference + (kSlack + Num<T>::kLift); }
+__device__ __forceinline__ bool too_far(float top, float scale, float reference) {   // (false where both are -inf)
+  return fmaf(top, scale, -reference) > kSlack + Num<T>::kLift;
+}
+template <typename T>
+__device__ __forceinline__ float new_reference(float top, float scale) { return __fmaf_ru(top, scale, -Num<T>::kLift); }
 
 // a box of the pool at {column, row in the page, operand and head, page, layer}
 __device__ __forceinline__ void tensor_g2s(uint32_t to, const CUtensorMap* map, int x, int row, int head, int page,

@@ -375,10 +375,10 @@ __device__ __forceinline__ bool wide_rows(const KvView& V, const AttendArgs& a, 
       float top4[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
       for (int c = 4; c < 64; ++c) top4[c & 3] = fmaxf(top4[c & 3], s[c]);
-      const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3])) * a.scale_log2;
-      const bool above = too_far<T>(top, m);
+      const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3]));
+      const bool above = too_far<T>(top, a.scale_log2, m);
       if (__any_sync(~0u, above)) {                  // (each row by itself: rows that are not there hold anything)
-        const float now = above ? top - Num<T>::kLift : m;
+        const float now = above ? new_reference<T>(top, a.scale_log2) : m;
         const float shrink = power(m - (now == -INFINITY ? 0.f : now));
         m = now;
         sum *= shrink;

@@ -1,0 +1,58 @@
+"""The paged key-value cache at its edges: scores far from zero, values that are not finite for every head dimension and
+row count, calls that are refused, streams that are not the current one."""
+import math
+
+import pytest
+import torch
+
+from paper_2312_11514_b200 import binding as B
+from paper_2312_11514_b200 import runtime as R
+
+import kv_util as K
+from test_gpu_kv import BF16, DEV, F16, attend, check_attention, ints, make, queries
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dim,heads,kv_heads", [(64, 2, 2), (80, 8, 1), (96, 3, 3), (128, 2, 1), (256, 2, 2), (256, 20, 1),
+                                                (64, 20, 1), (128, 20, 1)])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("power,steps", [
+    (24, [4, 8]), (24, [0, 4, 8, 12]), (24, [8, 4]), (26, [1, 3, 4]), (27, [1, 2]), (27, [0, 1]), (27, [2, 1, 3])])
+def test_scores_far_from_zero(dim, heads, kv_heads, dtype, power, steps):
+    """Scores of 2^power and a few units more (of the last place that fp32 has there), a tile of 64 keys for each of
+    `steps`: the products and their sums are exact, the scale is ln 2, so that weights are powers of two of the
+    differences, and no weight may leave fp16's range however the reference is rounded at that size.  The sequence stands in many
+    places (all but their last pages are the same ones), so that runs hold several of its tiles.
+
+    Bound: differences are multiples of 2 and at most 48, their product with scale log2(e) = 1 +- 2^-23 and the
+    exponential are off by 48 2^-23 + 2^-21 relative (2^-17 covers both); the rest as in kv_util.attention."""
+    tokens, page, unit, places, last = 64 * len(steps), 64, 2 ** (power - 23), 700, len(steps) - 1
+    g = torch.Generator(device=DEV)
+    g.manual_seed(dim + power)
+    pages = torch.zeros(1, last + places, 2, kv_heads, page, dim, dtype=dtype, device=DEV)
+    pages[0, :last + 1, 1].normal_(generator=g)
+    pages[0, :, 0, :, :, 0] = 2.0 ** (power // 2)
+    pages[0, :last + 1, 0, :, :, 1] = torch.tensor(steps, device=DEV, dtype=dtype)[:, None, None]
+    pages[0, last + 1:] = pages[0, last]
+    kv = R.KvCache(n_layers=1, n_heads=heads, n_kv_heads=kv_heads, head_dim=dim, n_pages=last + places, max_seqs=places,
+                   max_pages=last + 1, page_tokens=page, dtype=dtype, pages=pages, scale=math.log(2.0))
+    table = torch.arange(last + 1, dtype=torch.int32, device=DEV).repeat(places, 1)
+    table[:, last] += torch.arange(places, dtype=torch.int32, device=DEV)
+    kv.load(ints([tokens] * places), table, ints([1] * places))
+    q = torch.zeros(places, 1, heads, dim, dtype=dtype, device=DEV)
+    q[..., 0], q[..., 1] = 2.0 ** (power - power // 2), unit
+    out = attend(kv, q)
+    w = torch.tensor(steps, dtype=torch.float64, device=DEV).repeat_interleave(64) * unit
+    w = torch.exp2(w - w.max())
+    w = w / w.sum()
+    V = K.held(pages, 0, list(range(len(steps))), tokens, 1)
+    want = (w @ V).repeat_interleave(heads // kv_heads, 0)
+    A = (w @ V.abs()).repeat_interleave(heads // kv_heads, 0)
+    u, sub = K.U[dtype], 2.0 ** -32 if dtype == F16 else 0.0
+    rel = u + 2.0 ** -17 + (tokens + 64) * 2.0 ** -23
+    bound = u * want.abs() + rel * (1 + rel) * (A + want.abs()) + tokens * 2 * sub * V.abs().amax() + 2.0 ** -25
+    assert torch.isfinite(out).all()
+    worst = float(((out[:, 0].double() - want).abs() / bound).max())
+    assert worst <= 1, f"{worst} of the bound"
+    kv.close()
