@@ -336,7 +336,7 @@ kv_arrange_kernel(KvView v, const int32_t* from, const int32_t* src, const int32
   for (int c = c0 + kEarlyChunks * step; c < chunks; c += step) {
     int r, j;
     const int page = entry(c, &r, &j);
-    if (page >= 0) v.table_tmp[(size_t)r * v.max_pages + j] = page;
+    if (j < s_pages[r]) v.table_tmp[(size_t)r * v.max_pages + j] = page;   // (-2 too: it is read again below)
     count(page);
   }
   barrier();                                 // references are counted

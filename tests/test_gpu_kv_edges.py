@@ -56,3 +56,38 @@ def test_scores_far_from_zero(dim, heads, kv_heads, dtype, power, steps):
     worst = float(((out[:, 0].double() - want).abs() / bound).max())
     assert worst <= 1, f"{worst} of the bound"
     kv.close()
+
+
+@pytest.mark.parametrize("max_seqs,n_pages,max_pages,per_place", [(5, 30000, 9000, 1500), (40, 45000, 1700, 1000)])
+def test_bad_ids_behind_what_warps_hold_in_registers(max_seqs, n_pages, max_pages, per_place):
+    """Tables handled by one CTA and by a cluster: a page id out of range among the pages of the step under way, in a
+    chunk past those that stay in registers, is refused and changes nothing, whatever the scratch copy of the table held."""
+    page = 8
+    kv = R.KvCache(n_layers=1, n_heads=1, n_kv_heads=1, head_dim=64, n_pages=n_pages, max_seqs=max_seqs,
+                   max_pages=max_pages, page_tokens=page, max_new=4)
+    rows = [list(range(b * per_place, (b + 1) * per_place)) for b in range(max_seqs)]
+    lens, news = [per_place * page - b % 3 for b in range(max_seqs)], [1 + b % 4 for b in range(max_seqs)]
+    table = ints([r + [-1] * (max_pages - per_place) for r in rows])
+    ref = K.Tables(max_seqs, max_pages, n_pages, page, 4)
+    scratch = kv.workspace[kv.table.data_ptr() + 4 * kv.table.numel() - kv.workspace.data_ptr():
+                           kv.refs.data_ptr() - kv.workspace.data_ptr()]
+    assert scratch.numel() >= 4 * kv.table.numel()
+    for loaded in (False, True):                             # into an empty cache, and over one that is in use
+        if loaded:
+            kv.clear_status()
+            kv.load(ints(lens), table, ints(news))
+            ref.load(lens, rows, news)
+            assert kv.stats()["status"] == B.LIF_OK
+            ref.check(kv)
+        for b, j, bad in ((max_seqs - 1, per_place - 1, n_pages), (max_seqs - 1, per_place - 1, -1),
+                          (max_seqs - 1, per_place - 1, 2 ** 31 - 1), (max_seqs - 2, 700, -2 ** 31), (max_seqs - 1, 40, n_pages)):
+            wrong = table.clone()
+            wrong[b, j] = bad
+            scratch.fill_(0x7F)
+            kv.clear_status()
+            refused = kv.stats()["refused"]
+            kv.load(ints(lens), wrong, ints(news))
+            s = kv.stats()
+            assert s["status"] == B.LIF_ERR_INVALID_ARG and s["refused"] == refused + 1
+            ref.check(kv)
+    kv.close()
