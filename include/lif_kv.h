@@ -67,7 +67,8 @@ typedef struct {
   int32_t page_tokens;     /* power of two, 8 .. 256 */
   int32_t n_pages;         /* pages of the pool, 1 .. 2^24 */
   int32_t max_seqs;        /* places, 1 .. LIF_KV_MAX_SEQS */
-  int32_t max_pages;       /* pages a sequence may have; max_pages * page_tokens <= 2^30 */
+  int32_t max_pages;       /* pages a sequence may have; max_pages * page_tokens <= 2^30, and over all places, key-value
+                              heads and blocks of rows at most 2^31 - 2^26 tiles of 64 tokens */
   int32_t max_new;         /* tokens of one sequence in one step, 1 .. LIF_KV_MAX_NEW */
   int32_t window;          /* 0: a token sees itself and everything before it; w > 0: itself and the
                               w - 1 tokens before it */

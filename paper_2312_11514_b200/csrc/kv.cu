@@ -654,11 +654,13 @@ lif_status check_desc(const lif_kv_desc* d) {
   if (d->rope == LIF_ROPE_NONE ? d->rope_dims != 0 : (d->rope_dims < 2 || d->rope_dims > D || d->rope_dims % 2))
     return LIF_ERR_INVALID_ARG;
   if (d->rope != LIF_ROPE_NONE && !isfinite(d->rope_scale)) return LIF_ERR_INVALID_ARG;
-  // tiles are numbered in 32 bits
+  // Tiles are numbered in 32 bits.  Sums of a tile's number and a share of them (of 32 shares at least) stay below
+  // 2^31 too: kv_plan and the attention kernels' walk form them.
+  constexpr long long kMaxTiles = (1LL << 31) - (1LL << 26);
   const long long rows = (long long)(d->n_heads / d->n_kv_heads) * d->max_new;
   const long long per_block = 16 * kv_row_tiles(*d), blocks = (rows + per_block - 1) / per_block;
   const long long tiles = ((long long)d->max_pages * d->page_tokens + kKvTile - 1) / kKvTile;
-  if (tiles * d->max_seqs > 0x7fffffffLL / (d->n_kv_heads * blocks)) return LIF_ERR_INVALID_ARG;
+  if (tiles * d->max_seqs > kMaxTiles / (d->n_kv_heads * blocks)) return LIF_ERR_INVALID_ARG;
   return LIF_OK;
 }
 
@@ -790,7 +792,7 @@ lif_status lif_kv_create(const lif_kv_desc* desc, lif_kv** out) {
   int per_sm = 0;
   bool ok = cudaGetDevice(&kv->device) == cudaSuccess &&
             cudaDeviceGetAttribute(&kv->n_sm, cudaDevAttrMultiProcessorCount, kv->device) == cudaSuccess &&
-            kv_attention_configure(kv, &per_sm) && per_sm > 0;
+            kv_attention_configure(kv, &per_sm) && per_sm > 0 && kv->n_sm * per_sm >= 32;   // (kMaxTiles)
   v.ctas = ok ? kv->n_sm * per_sm < kKvMaxCtas ? kv->n_sm * per_sm : kKvMaxCtas : 0;
   ok = ok && cudaFuncSetAttribute(kv_reserve_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kReserveListMost * 4) == cudaSuccess &&
        cudaFuncSetAttribute(kv_arrange_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallPages * 4) == cudaSuccess &&
