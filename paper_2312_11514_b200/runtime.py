@@ -157,7 +157,9 @@ class KvCache:
     """A paged key-value cache for the attention between the FFN layers (include/lif_kv.h): owns its
     workspace (and the pool, unless ``pages`` is given) and the handle.  Tensors are checked here for
     device, type and shape; the calls run on ``stream``, by default the current stream of the cache's
-    device.  All calls of one cache are to be ordered (one stream, or events between streams).
+    device.  All calls of one cache are to be ordered (one stream, or events between streams).  An output
+    that a call makes itself (``q_out``, ``out`` left out) is memory of the call's stream: on another
+    stream it is to be used as any tensor of that stream is (an event, ``record_stream``).
 
     ``pages``: the pool, ``[n_layers][n_pages][2][n_kv_heads][page_tokens][head_dim]``; ``lens``,
     ``n_new``, ``table``, ``refs``: views of the tables on the device."""
@@ -229,6 +231,16 @@ class KvCache:
     def _on(self, stream):
         return torch._C._cuda_getCurrentRawStream(self._index) if stream is None else stream
 
+    def _new(self, stream):
+        # Memory of the stream that writes it: the current stream's may be a block that work pending there still uses.
+        if stream is None:
+            return torch.empty(self._queries, dtype=self.dtype, device=self.device)
+        if not isinstance(stream, torch.cuda.Stream):
+            at = B._stream(stream)
+            stream = torch.cuda.ExternalStream(at, self.device) if at else torch.cuda.default_stream(self.device)
+        with torch.cuda.stream(stream):
+            return torch.empty(self._queries, dtype=self.dtype, device=self.device)
+
     def _rows(self, name, t, shape):
         if t.get_device() != self._index or t.dtype is not self.dtype or t.shape != shape:
             self._expect(name, t, shape, contiguous=False)
@@ -252,7 +264,7 @@ class KvCache:
         Returns the normed and rotated queries (rows of tokens that are not there are not written)."""
         index, dtype, head = self._index, self.dtype, self._head
         if q_out is None:
-            q_out = torch.empty(self._queries, dtype=dtype, device=self.device)
+            q_out = self._new(stream)
         else:
             self._expect("q_out", q_out, self._queries)
         weights = None
@@ -278,7 +290,7 @@ class KvCache:
     def attention(self, layer: int, q: torch.Tensor, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         self._expect("q", q, self._queries)
         if out is None:
-            out = torch.empty_like(q)
+            out = self._new(stream)
         else:
             self._expect("out", out, self._queries)
         stream = torch._C._cuda_getCurrentRawStream(self._index) if stream is None else B._stream(stream)

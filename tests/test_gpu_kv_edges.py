@@ -91,3 +91,32 @@ def test_bad_ids_behind_what_warps_hold_in_registers(max_seqs, n_pages, max_page
             assert s["status"] == B.LIF_ERR_INVALID_ARG and s["refused"] == refused + 1
             ref.check(kv)
     kv.close()
+
+
+@pytest.mark.parametrize("given", ["object", "number", "default", "none"])
+def test_outputs_are_memory_of_the_stream_that_writes_them(given):
+    """The current stream holds back a write into a block that the caller has dropped; a call on another stream that
+    makes its own output may not be given that block."""
+    lens, news = [70, 33], [2, 2]
+    kv, rows, g = make(lens, news, heads=8, kv_heads=4, dim=128)
+    q, k, v = queries(kv, g), queries(kv, g, 4), queries(kv, g, 4)
+    side, busy = torch.cuda.Stream(), torch.cuda.Stream()
+    stream = {"object": side, "number": side.cuda_stream, "default": 0, "none": None}[given]
+    for call, right in ((lambda: kv.append(0, q, k, v, stream=stream), lambda out: torch.equal(out, q)),
+                        (lambda: kv.attention(0, q, stream=stream),
+                         lambda out: check_attention(kv, rows, lens, news, q, out) >= 0)):
+        call()                                               # (no allocation from the device below)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(busy):
+            held = [torch.empty_like(q) for _ in range(4)]
+            at = {t.data_ptr() for t in held}
+            torch.cuda._sleep(20_000_000)                    # ten milliseconds
+            for t in held:
+                t.fill_(3)
+            del held, t
+            out = call()
+            assert (out.data_ptr() in at) == (stream is None)     # the busy stream's own call may reuse its block
+        torch.cuda.synchronize()
+        assert right(out)
+    assert kv.stats()["status"] == B.LIF_OK
+    kv.close()
