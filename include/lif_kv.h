@@ -158,7 +158,7 @@ lif_status lif_kv_append(lif_kv* kv, int32_t layer, const lif_kv_rows* q, const 
  *   out[b][t][i] = sum_j w_j v_j / sum_j w_j,  w_j = exp(scale <q[b][t][i], k_j> - max_j ...),
  * j over the tokens that the position of token t sees.  dev_q and dev_out: [max_seqs][max_new]
  * [n_heads][head_dim], 16-byte aligned; rows t >= n_new[b] are neither read nor written.  dev_out may
- * not overlap dev_q.  What a token does not see never enters its result, infinities and NaN included
+ * not overlap dev_q (LIF_ERR_INVALID_ARG).  What a token does not see never enters its result, infinities and NaN included
  * (rows of a sequence's pages that no token sees may be read all the same).
  * The w_j are rounded to the cache's type: by half a unit in the last place, and with LIF_TYPE_F16 by up to 2^-32 of
  * the row's largest where they are below 2^-21 of it.  Scores scale <q, k> may be up to 10^8 in magnitude (beyond,

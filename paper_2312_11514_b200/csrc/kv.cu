@@ -701,6 +701,9 @@ uint64_t turn_fraction(double radians) {
   return s >= 9223372036854775808.0L ? (uint64_t)1 << 63 : (uint64_t)(int64_t)s;
 }
 
+// [max_seqs][max_new][n_heads][head_dim]
+size_t query_bytes(const lif_kv_desc& d) { return (size_t)d.max_seqs * d.max_new * d.n_heads * d.head_dim * 2; }
+
 lif_status enter(const lif_kv* kv) {
   if (!kv) return LIF_ERR_INVALID_ARG;
   int dev = -1;
@@ -890,6 +893,9 @@ lif_status lif_kv_append(lif_kv* kv, int32_t layer, const lif_kv_rows* q, const 
 lif_status lif_kv_attention(lif_kv* kv, int32_t layer, const void* dev_q, void* dev_out, void* stream) {
   if (!kv || !dev_q || !dev_out || layer < 0 || layer >= kv->desc.n_layers) return LIF_ERR_INVALID_ARG;
   if (!aligned(dev_q, 16) || !aligned(dev_out, 16)) return LIF_ERR_ALIGNMENT;
+  // A row of queries is read again by every CTA that has a piece of it, after others have written theirs.
+  const uintptr_t from = (uintptr_t)dev_q, to = (uintptr_t)dev_out;
+  if ((from < to ? to - from : from - to) < query_bytes(kv->desc)) return LIF_ERR_INVALID_ARG;
   const lif_status s = enter(kv);
   if (s != LIF_OK) return s;
   return done(launch_kv_attention(kv, layer, dev_q, dev_out, (cudaStream_t)stream));

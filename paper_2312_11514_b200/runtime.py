@@ -288,6 +288,9 @@ class KvCache:
         return q_out
 
     def attention(self, layer: int, q: torch.Tensor, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """q as `append` returns it; ``out`` of the same shape, in other memory.  Rows of tokens that are not
+        there are not written: in an output made here they hold anything, NaN included, and are to be
+        masked before sums over them."""
         self._expect("q", q, self._queries)
         if out is None:
             out = self._new(stream)

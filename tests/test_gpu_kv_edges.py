@@ -120,3 +120,23 @@ def test_outputs_are_memory_of_the_stream_that_writes_them(given):
         assert right(out)
     assert kv.stats()["status"] == B.LIF_OK
     kv.close()
+
+
+def test_attention_refuses_to_write_over_its_queries():
+    kv, rows, g = make([40, 9], [2, 1], heads=4, kv_heads=2)
+    q = queries(kv, g)
+    n, was = q.numel(), q.clone()
+    both = torch.zeros(3 * n, dtype=F16, device=DEV)
+    at = lambda i: both[i:i + n].view_as(q)
+    for a, b in ((q, q), (at(0), at(8)), (at(n - 8), at(0)), (at(n), at(8))):
+        with pytest.raises(B.LifError) as e:
+            kv.attention(0, a, out=b)
+        assert e.value.code == B.LIF_ERR_INVALID_ARG
+    assert torch.equal(q, was) and not both.any()
+    for i, j in ((0, 1), (1, 0), (2, 1)):                    # side by side
+        at(i * n).copy_(q)
+        out = at(j * n).fill_(7)
+        kv.attention(0, at(i * n), out=out)
+        check_attention(kv, rows, [40, 9], [2, 1], q, out)
+    assert kv.stats()["status"] == B.LIF_OK
+    kv.close()
