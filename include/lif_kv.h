@@ -148,7 +148,7 @@ lif_status lif_kv_reserve(lif_kv* kv, const int32_t* dev_n_new, void* stream);
 /* The new tokens' queries, keys and values of one layer: q and k through norm and rotation (positions
  * are places in the sequence: lens[b] - n_new[b] + t), k and v into the pages, q to dev_q_out
  * [max_seqs][max_new][n_heads][head_dim] (16-byte aligned; may be q->dev itself where q is laid out
- * so, and must not overlap it otherwise).  Rows t >= n_new[b] are neither used nor written.
+ * so; otherwise no row of q, k or v may lie in it: LIF_ERR_INVALID_ARG).  Rows t >= n_new[b] are neither used nor written.
  * norms: required (its weights too) with a norm, ignored without. */
 lif_status lif_kv_append(lif_kv* kv, int32_t layer, const lif_kv_rows* q, const lif_kv_rows* k,
                          const lif_kv_rows* v, const lif_kv_norms* norms, void* dev_q_out, void* stream);

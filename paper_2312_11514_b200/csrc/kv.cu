@@ -704,6 +704,20 @@ uint64_t turn_fraction(double radians) {
 // [max_seqs][max_new][n_heads][head_dim]
 size_t query_bytes(const lif_kv_desc& d) { return (size_t)d.max_seqs * d.max_new * d.n_heads * d.head_dim * 2; }
 
+// Does any row of an operand of append lie in the packed block of queries at `out`?
+bool touches(const lif_kv_rows& r, int heads, const lif_kv_desc& d, const void* out) {
+  const long long tokens = (long long)d.max_seqs * d.max_new, row = d.head_dim * 2;
+  const long long token = r.token_stride * 2, head = r.head_stride * 2, n = (long long)query_bytes(d);
+  const long long at = (long long)((uintptr_t)r.dev - (uintptr_t)out);          // of the block's first byte
+  if (at >= n || at + (tokens - 1) * token + (heads - 1) * head + row <= 0) return false;
+  for (int h = 0; h < heads; ++h) {
+    const long long b = at + h * head;               // this head's rows begin at b + t * token
+    const long long t = b + row > 0 ? 0 : token ? (-b - row) / token + 1 : tokens;   // the first that ends inside or behind
+    if (t < tokens && b + t * token < n) return true;
+  }
+  return false;
+}
+
 lif_status enter(const lif_kv* kv) {
   if (!kv) return LIF_ERR_INVALID_ARG;
   int dev = -1;
@@ -876,6 +890,12 @@ lif_status lif_kv_append(lif_kv* kv, int32_t layer, const lif_kv_rows* q, const 
     if (!aligned(r->dev, 16) || r->token_stride % 8 || r->head_stride % 8) return LIF_ERR_ALIGNMENT;
   }
   if (!aligned(dev_q_out, 16)) return LIF_ERR_ALIGNMENT;
+  const lif_kv_desc& d = kv->desc;
+  const bool in_place = q->dev == dev_q_out && (d.n_heads == 1 || q->head_stride == d.head_dim) &&
+                        (d.max_seqs * d.max_new == 1 || q->token_stride == (int64_t)d.n_heads * d.head_dim);
+  if ((!in_place && touches(*q, d.n_heads, d, dev_q_out)) || touches(*k, d.n_kv_heads, d, dev_q_out) ||
+      touches(*v, d.n_kv_heads, d, dev_q_out))
+    return LIF_ERR_INVALID_ARG;
   lif_kv_norms n = {};
   if (kv->desc.norm != LIF_NORM_NONE) {
     if (!norms || !norms->dev_q_weight || !norms->dev_k_weight) return LIF_ERR_INVALID_ARG;

@@ -140,3 +140,46 @@ def test_attention_refuses_to_write_over_its_queries():
         check_attention(kv, rows, [40, 9], [2, 1], q, out)
     assert kv.stats()["status"] == B.LIF_OK
     kv.close()
+
+
+@pytest.mark.parametrize("max_seqs,max_new,heads,kv_heads", [(3, 2, 4, 2), (1, 1, 4, 4), (1, 3, 1, 1), (5, 1, 6, 3)])
+def test_append_refuses_to_write_over_its_operands(max_seqs, max_new, heads, kv_heads):
+    """All ways to lay queries, keys and values beside and over the block of queries that comes out; refused exactly
+    where an element of theirs lies in it, unless the queries are that block."""
+    dim, tokens = 64, max_seqs * max_new
+    kv = R.KvCache(n_layers=1, n_heads=heads, n_kv_heads=kv_heads, head_dim=dim, n_pages=2 * max_seqs, max_seqs=max_seqs,
+                   max_new=max_new, page_tokens=8)
+    n, size = tokens * heads * dim, 24 * tokens * heads * dim
+    block = torch.zeros(size, dtype=F16, device=DEV)
+    base, out_at = block.data_ptr(), size // 2
+    out = set(range(out_at, out_at + n, 8))
+    far, seen = B.KvRows(base, 0, dim), set()                # n_heads * dim elements at most, at the beginning
+
+    def rows_of(r, count):
+        first = (r.dev - base) // 2
+        return {first + t * r.token_stride + h * r.head_stride + e
+                for t in range(tokens) for h in range(count) for e in range(0, dim, 8)}
+
+    for token in (0, heads * dim, (heads + 2 * kv_heads) * dim, 3 * heads * dim, dim, 5 * n):
+        for head in (dim, 3 * dim, tokens * dim, 0):
+            for start in (out_at, out_at + n, out_at - dim, out_at + 8, out_at - 8, out_at + n - 8, out_at - token,
+                          out_at - token * (tokens - 1) - head * (heads - 1) - dim, out_at - heads * dim, 0):
+                start = max(0, start)
+                for which, count in ((0, heads), (1, kv_heads), (2, kv_heads)):
+                    r = B.KvRows(base + 2 * start, token, head)
+                    if start + token * (tokens - 1) + head * (count - 1) + dim > size:
+                        continue
+                    packed = (tokens == 1 or token == heads * dim) and (heads == 1 or head == dim)
+                    allowed = not rows_of(r, count) & out or (which == 0 and start == out_at and packed)
+                    seen.add((which, allowed))
+                    args = [far, far, far]
+                    args[which] = r
+                    if allowed:
+                        B.lif_kv_append(kv.handle, 0, *args, None, base + 2 * out_at)
+                    else:
+                        with pytest.raises(B.LifError) as e:
+                            B.lif_kv_append(kv.handle, 0, *args, None, base + 2 * out_at)
+                        assert e.value.code == B.LIF_ERR_INVALID_ARG
+    assert len(seen) == 6
+    assert kv.stats()["status"] == B.LIF_OK and not block.any()          # (no step is under way: nothing was written)
+    kv.close()
