@@ -183,3 +183,103 @@ def test_append_refuses_to_write_over_its_operands(max_seqs, max_new, heads, kv_
     assert len(seen) == 6
     assert kv.stats()["status"] == B.LIF_OK and not block.any()          # (no step is under way: nothing was written)
     kv.close()
+
+
+def _poison(kv):
+    bad = torch.tensor([float("nan"), float("inf"), -float("inf"), torch.finfo(kv.dtype).min], device=DEV).to(kv.dtype)
+    return bad[torch.arange(kv.pages.numel(), device=DEV) % 4].view_as(kv.pages)
+
+
+@pytest.mark.parametrize("dim,heads,kv_heads", [
+    (64, 6, 3), (80, 4, 2), (96, 4, 2), (128, 4, 2), (256, 4, 2),         # up to 16 rows a key-value head
+    (80, 8, 2), (96, 8, 2), (256, 8, 2),                                  # two tiles of rows,
+    (80, 20, 2), (96, 20, 2), (256, 20, 2),                               # four,
+    (80, 32, 2), (96, 32, 2), (256, 32, 2),                               # eight (256: two blocks of four)
+    (80, 60, 2), (96, 60, 2),                                             # two blocks of eight
+    (64, 32, 2), (64, 60, 2), (128, 32, 2), (128, 60, 2)])                # the tensor cores' blocks
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("window", [0, 20])
+def test_values_that_are_not_finite(dim, heads, kv_heads, dtype, window):
+    """Infinities, NaN and the type's lowest value where no token sees them, then in the last token's row (which the tokens
+    of its step before it do not see), then in the row that is the first token's last before it leaves the window (which the
+    tokens behind it do not see): every token that does not see them as the formula has it, every one that does not finite."""
+    lens, news = [70, 64, 9, 40, 200, 0], [4, 3, 5, 1, 2, 0]
+    kv, rows, g = make(lens, news, dtype=dtype, dim=dim, heads=heads, kv_heads=kv_heads, window=window, seed=dim + heads)
+    q = queries(kv, g)
+    clean, fill = kv.pages.clone(), _poison(kv)
+    want = attend(kv, q)
+    check_attention(kv, rows, lens, news, q, want, window=window)
+    first = [max(0, L - n + 1 - window) if window else 0 for L, n in zip(lens, news)]
+    held = torch.zeros(kv.pages.shape[1], 16, dtype=torch.bool, device=DEV)
+    for b, L in enumerate(lens):
+        for p in range(first[b], L):
+            held[rows[b][p // 16], p % 16] = True
+    unseen = torch.where(held[None, :, None, None, :, None], clean, fill)
+
+    def put(b, p):
+        kv.pages[0, rows[b][p // 16], :, :, p % 16] = fill[0, rows[b][p // 16], :, :, p % 16]
+
+    def check(out, b, t0, t1):
+        """Tokens t0 .. t1-1 of place b."""
+        if t1 > t0:
+            y, bound = K.attention(q[b, t0:t1], clean, 0, rows[b], lens[b] - news[b] + t1, t1 - t0, window)
+            assert ((out[b, t0:t1].double() - y).abs() <= bound).all()
+
+    kv.pages.copy_(unseen)
+    assert torch.equal(attend(kv, q), want)
+    for b, L in enumerate(lens):
+        if L:
+            put(b, L - 1)
+    out = attend(kv, q)
+    for b, n in enumerate(news):
+        check(out, b, 0, n - 1)
+        assert n == 0 or not torch.isfinite(out[b, n - 1]).any()
+        assert (out[b, n:] == 7).all()
+    if window:
+        kv.pages.copy_(unseen)
+        leaves = [b for b, L in enumerate(lens) if L - news[b] + 1 > window]
+        assert leaves
+        for b in leaves:
+            put(b, first[b])
+        out = attend(kv, q)
+        for b in leaves:
+            check(out, b, 1, news[b])
+            assert not torch.isfinite(out[b, 0]).any()
+    assert kv.stats()["status"] == B.LIF_OK
+    kv.close()
+
+
+@pytest.mark.parametrize("dim,heads,kv_heads,max_new", [(64, 4, 2, 1), (128, 8, 1, 4), (80, 6, 2, 3)])
+def test_few_places_in_use_far_apart(dim, heads, kv_heads, max_new):
+    """1024 places of which a handful hold sequences, tables and attention."""
+    live = {0: 90, 1: 7, 300: 700, 511: 64, 512: 65, 1000: 1, 1023: 333}
+    lens = [live.get(b, 0) for b in range(1024)]
+    news = [min(live.get(b, 0), max_new - b % 2 if max_new > 1 else 1) for b in range(1024)]
+    kv, rows, g = make(lens, news, heads=heads, kv_heads=kv_heads, dim=dim)
+    q = queries(kv, g)
+    check_attention(kv, rows, lens, news, q, attend(kv, q))
+    kv.close()
+
+
+@pytest.mark.parametrize("dim,heads,kv_heads", [(64, 8, 8), (128, 16, 2), (96, 8, 2), (256, 4, 2)])
+def test_single_tokens_through_a_cache_for_pieces_of_a_prompt(dim, heads, kv_heads):
+    """A prompt in steps of 64, a shorter last one, then single tokens: the same cache, every step's attention."""
+    kv = R.KvCache(n_layers=1, n_heads=heads, n_kv_heads=kv_heads, head_dim=dim, n_pages=40, max_seqs=3, page_tokens=16,
+                   max_new=64)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(dim)
+    ref = K.Tables(3, kv.max_pages, 40, 16, 64)
+    for n in ([64, 64, 0], [64, 9, 40], [20, 1, 1], [1, 1, 1], [1, 0, 1], [1, 1, 5]):
+        kv.reserve(ints(n))
+        assert ref.reserve(n)[0] is None
+        q, k, v = queries(kv, g), queries(kv, g, kv_heads), queries(kv, g, kv_heads)
+        q2 = kv.append(0, q, k, v, q_out=torch.full_like(q, 7))
+        for b in range(3):
+            assert torch.equal(q2[b, :n[b]], q[b, :n[b]]) and (q2[b, n[b]:] == 7).all()
+            if n[b]:
+                for what, x in ((0, k), (1, v)):
+                    got = K.held(kv.pages, 0, ref.rows[b], ref.lens[b], what)[:, ref.lens[b] - n[b]:]
+                    assert torch.equal(got, x[b, :n[b]].transpose(0, 1).double())
+        check_attention(kv, ref.rows, ref.lens, n, q, attend(kv, q))
+    ref.check(kv)
+    kv.close()
