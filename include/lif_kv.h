@@ -23,7 +23,8 @@
  * refused as a whole and changes nothing but what its description says.
  * All calls of one cache use its workspace: they are to be ordered one behind the other (one stream,
  * or events between streams).  Different caches are independent.  The device that was current at
- * lif_kv_create has to be current in every later call (LIF_ERR_STATE otherwise).
+ * lif_kv_create has to be current in every later call with a stream and in lif_kv_get_stats
+ * (LIF_ERR_STATE otherwise, and nothing is done).
  *
  * Sequences have places 0 .. max_seqs-1.  Place b holds `lens[b]` tokens, of which the last
  * `n_new[b]` are the tokens of the step under way; a free place has length 0.  Token p of it is row

@@ -115,7 +115,6 @@ template <> struct Num<__half> {
     __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<uint32_t*>(&h);
   }
-  static __device__ __forceinline__ float to1(unsigned short v) { return __half2float(__ushort_as_half(v)); }
   static constexpr uint32_t kExponent = 0x7c007c00u;   // all ones: infinite or NaN
   static constexpr float kLift = 7.f;                  // of a softmax's weights (kv_attention.cuh)
 };
@@ -125,7 +124,6 @@ template <> struct Num<__nv_bfloat16> {
     __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<uint32_t*>(&h);
   }
-  static __device__ __forceinline__ float to1(unsigned short v) { return __bfloat162float(__ushort_as_bfloat16(v)); }
   static constexpr uint32_t kExponent = 0x7f807f80u;
   static constexpr float kLift = 0.f;
 };

@@ -157,7 +157,9 @@ class KvCache:
     """A paged key-value cache for the attention between the FFN layers (include/lif_kv.h): owns its
     workspace (and the pool, unless ``pages`` is given) and the handle.  Tensors are checked here for
     device, type and shape; the calls run on ``stream``, by default the current stream of the cache's
-    device.  All calls of one cache are to be ordered (one stream, or events between streams).  An output
+    device, which has to be the current device (``stats`` and ``close`` see to it themselves; others
+    raise LIF_ERR_STATE).  All calls of one cache are to be ordered (one stream, or events between streams),
+    and tensors given stay until the call's stream is done with them.  An output
     that a call makes itself (``q_out``, ``out`` left out) is memory of the call's stream: on another
     stream it is to be used as any tensor of that stream is (an event, ``record_stream``).
 
