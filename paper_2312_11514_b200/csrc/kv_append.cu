@@ -12,8 +12,9 @@
 // 2^-34 of a turn at position 2^30, where an fp32 product would be off by whole turns; sincospif then
 // takes the fraction, reduced, in fp32.  Norm and rotation are fp32; one rounding at the end.
 // Bound: latency for a decode step's few tokens (3.1 us for 8 tokens of 192 rows of 64: length and page are
-// two dependent round trips, the rows travel beside the second), instructions for long pieces of a prompt
-// (25 MB in 7.4 us, 52% of measured HBM; the first version took 9.0).
+// two dependent round trips, the rows travel beside the second); latency too for long pieces of a prompt, where half
+// of the stalls are loads and 37% of the issue slots are used: queries are fetched one row ahead, keys and
+// values past a group's first not at all (25 MB in 7.4 us, 52% of measured HBM; the first version took 9.0).
 #include "kv_internal.cuh"
 
 namespace lif {

@@ -13,7 +13,7 @@
 // Every CTA begins with a run of its own; where the work is long these cover most of it and the
 // rest is taken in short runs by whoever is free: CTAs with equal work differ by a fifth in time (memory is nearer to
 // some pages than to others), and 64 sequences of 56 heads went from 451 to 360 us.  A head that a run's end cuts is
-// finished by kv_join_kernel from the pieces' {max, sum, unnormalised output}.  Which run holds which tiles
+// finished by kv_join_kernel from the pieces' {reference, sum, unnormalised output}.  Which run holds which tiles
 // does not depend on who takes it, and pieces are joined in their order: the same bits every time.
 //
 // Loads.  One warp feeds the others: it walks the run, reads 32 page ids at a time and moves keys and
@@ -24,7 +24,7 @@
 // shared memory before use (whatever they hold, 0 times it is not 0), the scores replaced by -inf.
 //
 // Products.  Of 64 keys each of WK warps takes 64 / WK, of the rows each of WR warps 16, and keeps a
-// running maximum, sum and output of its own (mma m16n8k16): between two tiles no warp waits for another,
+// running reference (kv_attention.cuh), sum and output of its own (mma m16n8k16): between two tiles no warp waits for another,
 // and the weights stay in registers from the first product to the second.  The WK warps of a row
 // are summed when the head ends.
 //
@@ -170,7 +170,7 @@ kv_attention_kernel(const __grid_constant__ KvMaps maps, KvView V, AttendArgs a)
   extern __shared__ __align__(1024) unsigned char smem[];
   unsigned char* queries = smem + S::kStages * S::kStage;
   unsigned char* scratch = queries + 2 * S::kQuerySlot;
-  float2* stats = reinterpret_cast<float2*>(scratch + S::kScratch);            // [rows][WK] maximum, sum
+  float2* stats = reinterpret_cast<float2*>(scratch + S::kScratch);            // [rows][WK] reference, sum
   StageInfo* info = reinterpret_cast<StageInfo*>(scratch + S::kScratch + S::kRows * WK * 8);
   Barriers* bars = reinterpret_cast<Barriers*>(info + S::kMaxStages);
   static_assert(sizeof(Barriers) <= 256, "");

@@ -43,7 +43,7 @@ struct KvView {
                            // {place, its first tile, tokens, new tokens} at the run's first tile
   int4 *joins;             // [max_runs] {first run, last run << 16; place; head << 16, row block; new tokens}
   const uint64_t* turns;   // [rope_dims/2] 2^64ths of a turn per position
-  float* partials;         // [2 * max_runs][slot_rows] {[head_dim], max, sum, -, -}
+  float* partials;         // [2 * max_runs][slot_rows] {[head_dim], reference, sum, -, -}
   int max_seqs, max_pages, n_pages, max_new, page_shift, window;
   int n_heads, n_kv_heads, group, head_dim, rows_per_block, ctas;
   int max_runs, slot_rows, slot_floats;
